@@ -1,4 +1,5 @@
-"""ctypes binding of libcts.so (include/cts.h, include/cts_compress.h).
+"""ctypes binding of libcts.so (include/cts.h, include/cts_compress.h,
+include/cts_block.h).
 
 Argument marshalling only: shapes, dtypes and devices are checked, raw
 device pointers and the current HIP stream are handed to the C library, and
@@ -51,7 +52,10 @@ EXPORTED = ("cts_status_string", "cts_workspace_size", "cts_workspace_size_uncom
             "cts_apply_multi_packed",
             # include/cts_compress.h
             "cts_jd_workspace_size", "cts_jd_cluster_workspace_size", "cts_lora_norms2", "cts_jd_full",
-            "cts_jd_diag", "cts_jd_sigma", "cts_jd_cluster")
+            "cts_jd_diag", "cts_jd_sigma", "cts_jd_cluster",
+            # include/cts_block.h
+            "cts_kv_write", "cts_kv_read", "cts_kv_attention_workspace_size", "cts_kv_attention", "cts_block_norm",
+            "cts_rotary")
 N_STAGE_EVENTS = 6
 
 
@@ -64,6 +68,18 @@ class CtsError(RuntimeError):
 class JdProblem(ctypes.Structure):
     _fields_ = [("n", ctypes.c_int32), ("d_out", ctypes.c_int32), ("d_in", ctypes.c_int32),
                 ("r_lora", ctypes.c_int32), ("r", ctypes.c_int32)]
+
+
+class KvCacheArrays(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("k_codes", ctypes.c_void_p), ("k_scales", ctypes.c_void_p),
+                ("v_codes", ctypes.c_void_p), ("v_scales", ctypes.c_void_p)]
+
+
+class AttnProblem(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("B", ctypes.c_int32), ("n_q_heads", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("max_q", ctypes.c_int32), ("max_kv", ctypes.c_int32),
+                ("window", ctypes.c_int32), ("dtype", ctypes.c_int32), ("scale", ctypes.c_float)]
 
 
 class Problem(ctypes.Structure):
@@ -143,6 +159,20 @@ def lib() -> ctypes.CDLL:
                 L.cts_jd_cluster.argtypes = [jp, i32, vp, vp, vp, vp, vp, vp, ctypes.POINTER(i32), i32, i32,
                                              i32, vp, vp, vp, vp, ctypes.POINTER(i32), vp, sz, vp]
                 L.cts_jd_cluster.restype = ctypes.c_int
+                cp, ap, i64 = ctypes.POINTER(KvCacheArrays), ctypes.POINTER(AttnProblem), ctypes.c_int64
+                L.cts_kv_write.argtypes = [cp, i32, vp, i64, vp, i64, vp, i32, vp]
+                L.cts_kv_write.restype = ctypes.c_int
+                L.cts_kv_read.argtypes = [cp, i32, vp, vp, i64, vp, i64, i32, vp]
+                L.cts_kv_read.restype = ctypes.c_int
+                L.cts_kv_attention_workspace_size.argtypes = [ap, cp]
+                L.cts_kv_attention_workspace_size.restype = sz
+                L.cts_kv_attention.argtypes = [ap, cp, vp, i64, vp, vp, vp, vp, i64, vp, sz, vp]
+                L.cts_kv_attention.restype = ctypes.c_int
+                L.cts_block_norm.argtypes = [i32, i32, i32, vp, i64, vp, i64, vp, vp, i64, fl, fl, vp, vp, i64, vp, i64, vp]
+                L.cts_block_norm.restype = ctypes.c_int
+                L.cts_rotary.argtypes = [i32, i32, i32, i32, i32, i32, vp, i64, vp, i64, vp, vp, i32, vp, i32,
+                                         ctypes.POINTER(i32), i32, vp, i64, vp, i64, vp]
+                L.cts_rotary.restype = ctypes.c_int
                 _lib = L
     return _lib
 

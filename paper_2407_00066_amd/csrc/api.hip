@@ -21,6 +21,7 @@
 
 #include "cts.h"
 #include "cts_internal.h"
+#include "host_checks.h"
 
 // Scratch memory of cts_apply_noalloc: one static array per device (each
 // GPU the library runs on holds its own copy until the process ends); it
@@ -30,6 +31,9 @@ __device__ __align__(256) unsigned char scratch[CTS_NOALLOC_SCRATCH_BYTES];
 namespace {
 
 using cts::Tile;
+using cts::misaligned;
+using cts::overlap;
+using cts::Range;
 
 constexpr size_t kAlign = 256;
 size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
@@ -375,20 +379,6 @@ bool bucket_layout(int T, int n, int K, BucketLayout* L) {
   L->cseg = off;    off = align_up(off + 4ull * (cts::max_seg_tiles(T, K) + 1));
   L->total = off;
   return true;
-}
-
-struct Range { const void* p; size_t bytes; };
-
-// Every float array is read or written in 16-byte vectors: its address must be
-// a multiple of 16 (ids: of 4).
-bool misaligned(const void* ptr, uintptr_t a) {
-  return (reinterpret_cast<uintptr_t>(ptr) & (a - 1)) != 0;
-}
-
-bool overlap(Range a, Range b) {
-  if (!a.p || !b.p || !a.bytes || !b.bytes) return false;
-  const uintptr_t a0 = reinterpret_cast<uintptr_t>(a.p), b0 = reinterpret_cast<uintptr_t>(b.p);
-  return a0 < b0 + b.bytes && b0 < a0 + a.bytes;
 }
 
 // y must not overlap any input or the workspace; the workspace must not
