@@ -20,8 +20,10 @@ namespace {
 
 constexpr int kRowTile = 16;       // query rows of a tile
 constexpr int kUnit = 32;          // tokens of a step
-constexpr int kWaves = 4;
-constexpr int kThreads = 64 * kWaves;
+constexpr int kSmallRows = 64;     // rows of a sequence that the 16-row tiles are for
+constexpr int kRuns = 4096;        // waves that a batch's steps are dealt out to: 16 for every compute unit
+constexpr int kMinRun = 4;         // steps of a run, at least
+constexpr int kJoinThreads = 256;
 
 __device__ __forceinline__ uint32_t fp4_pair(uint32_t w, float unit, int byte) {
   switch (byte) {
@@ -79,42 +81,62 @@ template <int NS> __device__ __forceinline__ void split(const float* f, bf16x8* 
 }
 
 struct Tile {                      // what a 16-row tile of a sequence covers
-  int q0, rows, row0;              // the sequence's first query row, its rows (query x head of the group), the tile's first
+  int b, q0, rows, row0;           // the sequence, its first query row, its rows (query x head of the group), the tile's first
   int first_pos;                   // position of the sequence's first query
-  int lo, hi;                      // tokens that some row of the tile sees, [lo, hi)
+  int lo, hi;                      // tokens that some row of the tile sees, [lo, hi); lo a multiple of a step
+  int steps;                       // steps of kUnit tokens (one where nothing is seen); 0: no such rows
 };
 
-// false: no rows here
-__device__ __forceinline__ bool tile_of(const AttnParams& p, int b, int sub, Tile* t) {
-  int q0 = b, q1 = b + 1;
-  if (p.q_start) {
-    q0 = min(max(p.q_start[b], 0), p.T);
-    q1 = min(max(p.q_start[b + 1], q0), p.T);
-  }
-  const int nq = q1 - q0, len = min(max(p.kv_len[b], 0), p.max_kv);
-  t->q0 = q0;
-  t->rows = min(nq, p.max_q) * p.group;
-  t->row0 = sub * kRowTile;
-  if (t->row0 >= t->rows) return false;
-  t->first_pos = len - nq;
-  const int j0 = t->row0 / p.group, j1 = (min(t->rows, t->row0 + kRowTile) - 1) / p.group;
-  t->hi = max(0, t->first_pos + j1 + 1);
-  t->lo = p.window ? max(0, t->first_pos + j0 - p.window + 1) & ~(kUnit - 1) : 0;
-  return true;
+struct Queries { int q0, n; };     // a sequence's query rows
+__device__ __forceinline__ Queries queries_of(const AttnParams& p, int b) {
+  if (!p.q_start) return {b, 1};
+  const int q0 = min(max(p.q_start[b], 0), p.T);
+  return {q0, min(max(p.q_start[b + 1], q0), p.T) - q0};
 }
 
-__device__ __forceinline__ int pieces_of(const AttnParams& p, const Tile& t) {
-  return t.hi > t.lo ? (t.hi - t.lo + p.chunk - 1) / p.chunk : 1;
+__device__ __forceinline__ Tile tile_of(const AttnParams& p, int b, int sub) {
+  Tile t;
+  const Queries q = queries_of(p, b);
+  const int len = min(max(p.kv_len[b], 0), p.max_kv);
+  t.b = b;
+  t.q0 = q.q0;
+  t.rows = min(q.n, p.max_q) * p.group;
+  t.row0 = sub * kRowTile;
+  t.first_pos = len - q.n;
+  const int j0 = t.row0 / p.group, j1 = (min(t.rows, t.row0 + kRowTile) - 1) / p.group;
+  t.hi = max(0, t.first_pos + j1 + 1);
+  t.lo = p.window ? max(0, t.first_pos + j0 - p.window + 1) & ~(kUnit - 1) : 0;
+  t.steps = t.row0 < t.rows ? max(1, (t.hi - t.lo + kUnit - 1) / kUnit) : 0;
+  return t;
 }
 
-template <typename TQ> __device__ __forceinline__ void store_out(TQ* o, const float* f);
-template <> __device__ __forceinline__ void store_out<float>(float* o, const float* f) {
-  reinterpret_cast<float4*>(o)[0] = make_float4(f[0], f[1], f[2], f[3]);
-  reinterpret_cast<float4*>(o)[1] = make_float4(f[4], f[5], f[6], f[7]);
+// The tiles of the sequences with few rows: tile `index` is sub-tile index %
+// subs of sequence index / subs (steps 0 for the others).
+__device__ __forceinline__ Tile small_tile(const AttnParams& p, int index) {
+  const int b = p.subs == 1 ? index : index / p.subs;
+  Tile t = tile_of(p, b, index - b * p.subs);
+  if (t.rows > kSmallRows) t.steps = 0;
+  return t;
 }
-template <> __device__ __forceinline__ void store_out<bf16_t>(bf16_t* o, const float* f) {
-  *reinterpret_cast<uint4*>(o) = make_uint4(f32_to_bf16_pair(f[0], f[1]), f32_to_bf16_pair(f[2], f[3]),
-                                            f32_to_bf16_pair(f[4], f[5]), f32_to_bf16_pair(f[6], f[7]));
+
+__device__ __forceinline__ Tile uniform(Tile t) {      // what every lane holds alike, in scalar registers
+  return {__builtin_amdgcn_readfirstlane(t.b),  __builtin_amdgcn_readfirstlane(t.q0),
+          __builtin_amdgcn_readfirstlane(t.rows), __builtin_amdgcn_readfirstlane(t.row0),
+          __builtin_amdgcn_readfirstlane(t.first_pos), __builtin_amdgcn_readfirstlane(t.lo),
+          __builtin_amdgcn_readfirstlane(t.hi), __builtin_amdgcn_readfirstlane(t.steps)};
+}
+
+// N (4 or 8) elements
+template <int N> __device__ __forceinline__ void store_out(float* o, const float* f) {
+#pragma unroll
+  for (int i = 0; i < N; i += 4) *reinterpret_cast<float4*>(o + i) = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
+}
+template <int N> __device__ __forceinline__ void store_out(bf16_t* o, const float* f) {
+  const uint32_t a = f32_to_bf16_pair(f[0], f[1]), b = f32_to_bf16_pair(f[2], f[3]);
+  if constexpr (N == 8)
+    *reinterpret_cast<uint4*>(o) = make_uint4(a, b, f32_to_bf16_pair(f[4], f[5]), f32_to_bf16_pair(f[6], f[7]));
+  else
+    *reinterpret_cast<uint2*>(o) = make_uint2(a, b);
 }
 
 template <typename TQ> __device__ __forceinline__ void load_q(const TQ* q, float* f);
@@ -133,47 +155,41 @@ template <> __device__ __forceinline__ void load_q<bf16_t>(const bf16_t* q, floa
   }
 }
 
-// One step's codes and scales as a lane holds them, of two groups of 16 tokens.
-template <int D> struct Raw {
-  static constexpr int KW = D / 32;              // words of keys a lane holds: d/4 elements of one token
-  static constexpr int NC = D > 128 ? 2 : 1;     // 16-byte pieces of values: 8 elements of 4 tokens each
-  uint32_t k[2][KW], ks[2];
-  uint4 v[2][NC];
-  uint32_t vs[2][NC];
+// What a wave holds of a tile: sums, and for its query row n the running maximum
+// and (over the lane's own tokens) length.
+template <int D> struct State {
+  static constexpr int NC = D > 128 ? 2 : 1;     // 16-byte pieces of values a lane takes: 8 elements of 4 tokens each
+  static constexpr int NB = D == 64 ? 4 : 8;     // elements of a piece that are the lane's (D = 64: lanes n and n + 8 share)
+  f32x4 o[NC][NB];
+  float m, l;
+  // sum o[c][e][i] of lane 16 g + n is row n's element
+  static __device__ __forceinline__ int element(int g, int c, int i) {
+    const int r = 4 * g + i;
+    return D == 64 ? 8 * (r & 7) + 4 * (r >> 3) : 8 * (r + 16 * c);
+  }
 };
 
-// A workgroup takes a piece of one tile's tokens for one key/value head; its
-// waves take steps of 32 tokens in turn, each with a softmax of its own, joined
-// at the end.
+// The tile's steps [s0, s1) for key/value head h, by one wave.
 template <int D, typename TQ>
-__global__ __launch_bounds__(kThreads) void attn_rows_kernel(AttnParams p) {
+__device__ __forceinline__ void attend(const AttnParams& p, const Tile& t, int h, int s0, int s1, State<D>& st) {
   constexpr int NS = sizeof(TQ) == 4 ? 3 : 1;
-  constexpr int KS = D / 32;                     // steps of the first product
-  constexpr int NC = Raw<D>::NC;
-  constexpr int NB = D == 64 ? 4 : 8;            // elements a lane takes of its piece
-  __shared__ float lds_o[kWaves][kRowTile][D + 4];
-  __shared__ float lds_m[kWaves][kRowTile], lds_l[kWaves][kRowTile];
-  int id = blockIdx.x;
-  const int piece = id % p.pieces; id /= p.pieces;
-  const int h = id % p.c.heads; id /= p.c.heads;
-  const int sub = id % p.subs, b = id / p.subs;
-  Tile t;
-  if (!tile_of(p, b, sub, &t)) return;
-  const int n_pieces = pieces_of(p, t);
-  if (piece >= n_pieces) return;
-  const int t0 = t.lo + piece * p.chunk, t1 = min(t.hi, t0 + p.chunk);
-
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int n = lane & 15, g = lane >> 4;
+  constexpr int KS = D / 32;                     // steps of the first product; words of keys a lane holds
+  constexpr int NC = State<D>::NC, NB = State<D>::NB;
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int row = t.row0 + n;
   const bool live = row < t.rows;
-  const int pos = live ? t.first_pos + row / p.group : -1;              // sees tokens first .. pos
+  const int query = row / p.group;
+  const int pos = live ? t.first_pos + query : -1;                      // sees tokens first .. pos
   const int first = p.window ? pos - p.window + 1 : 0;
+  auto seen = [&](int at, int i, int j) {
+    const int tok = at + 16 * i + 4 * g + j;
+    return tok <= pos && tok >= first;
+  };
 
   bf16x8 qf[KS][NS];
   {
-    const TQ* q = static_cast<const TQ*>(p.q) + (live ? (t.q0 + row / p.group) * p.ldq +
-                                                 static_cast<int64_t>(h * p.group + row % p.group) * D : 0);
+    const TQ* q = static_cast<const TQ*>(p.q) + (live ? (t.q0 + query) * p.ldq +
+                                                 static_cast<int64_t>(h * p.group + row - query * p.group) * D : 0);
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       float f[8] = {0, 0, 0, 0, 0, 0, 0, 0};
@@ -181,293 +197,497 @@ __global__ __launch_bounds__(kThreads) void attn_rows_kernel(AttnParams p) {
       split<NS>(f, qf[s]);
     }
   }
-
-  f32x4 o[NC][NB];
 #pragma unroll
   for (int c = 0; c < NC; ++c)
 #pragma unroll
-    for (int e = 0; e < NB; ++e) o[c][e] = f32x4{0, 0, 0, 0};
-  float m = -INFINITY, l = 0.0f;
+    for (int e = 0; e < NB; ++e) st.o[c][e] = f32x4{0, 0, 0, 0};
+  st.m = -INFINITY;
+  st.l = 0.0f;
+  if (t.hi <= t.lo) return;                                             // nothing is seen
 
-  const int page_size = 1 << p.c.page_shift;
-  const int steps = t1 > t0 ? (t1 - t0 + kUnit - 1) / kUnit : 0;
   // tokens that every live row of the tile sees
   const int all_hi = t.first_pos + t.row0 / p.group + 1;
   const int all_lo = p.window ? t.first_pos + (min(t.rows, t.row0 + kRowTile) - 1) / p.group - p.window + 1 : 0;
 
-  auto load = [&](int step, Raw<D>& r) {
+  // Page numbers of the next 32 steps, two groups of 16 tokens each, a lane one:
+  // a step's addresses do not wait for its own look-up.  A group past the last
+  // seen token is not looked up: the last group's codes stand in for it, masked.
+  const int last16 = (t.hi - 1) & ~15;
+  int pages = 0;
+  auto look_up = [&](int s) {
+    const int tok = min(t.lo + s * kUnit + 16 * lane, last16);
+    pages = p.table[static_cast<int64_t>(t.b) * p.max_pages + (tok >> p.c.page_shift)];
+  };
+  // token offset of a group's first token within the cache's heads, and whether its page is outside the cache
+  struct Group { int64_t base; bool bad; };
+  const int page_mask = (1 << p.c.page_shift) - 1;
+  auto group_of = [&](int s, int i) -> Group {
+    const int page = __builtin_amdgcn_readlane(pages, 2 * ((s - s0) & 31) + i);
+    const int tok = min(t.lo + s * kUnit + 16 * i, last16);
+    const bool bad = static_cast<uint32_t>(page) >= static_cast<uint32_t>(p.c.n_pages);
+    return {((static_cast<int64_t>(bad ? 0 : page) * p.c.heads + h) << p.c.page_shift) + (tok & page_mask), bad};
+  };
+  const uint32_t k_at = n * (D / 2) + g * (D / 8), ks_at = n * (D / 32) + (D == 64 ? g >> 1 : D == 128 ? g : 2 * g);
+  uint32_t v_at[NC], vs_at[NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const int eighth = (n & (D / 8 - 1)) + 16 * c;
+    v_at[c] = (g * (D / 8) + eighth) * 16;
+    vs_at[c] = (g * (D / 32) + eighth / 4) * 4;
+  }
+  uint32_t k[2][KS], ks[2], vs[2][NC];
+  uint4 v[2][NC];
+  Group gr[2];
+  auto load_k = [&](int s) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      // a group past the piece's end lies past what is seen: the last group's codes stand in, masked
-      const int tok = min(t0 + step * kUnit + 16 * i, (t1 - 1) & ~15);
-      const int page = __builtin_amdgcn_readfirstlane(p.table[static_cast<int64_t>(b) * p.max_pages + (tok >> p.c.page_shift)]);
-      const bool bad = static_cast<uint32_t>(page) >= static_cast<uint32_t>(p.c.n_pages);
-      const int64_t base = ((static_cast<int64_t>(bad ? 0 : page) * p.c.heads + h) << p.c.page_shift) + (tok & (page_size - 1));
-      const uint8_t* kc = p.c.kc + base * (D / 2) + n * (D / 2) + g * (D / 8);
-      const uint8_t* ks = p.c.ks + base * (D / 32) + n * (D / 32);
-      const uint8_t* vc = p.c.vc + base * (D / 2);
-      const uint8_t* vs = p.c.vs + base * (D / 32);
+      gr[i] = group_of(s, i);
+      const uint8_t* kc = p.c.kc + gr[i].base * (D / 2);
+      const uint8_t* sc = p.c.ks + gr[i].base * (D / 32);
       if constexpr (D == 64) {
-        const uint2 w = *reinterpret_cast<const uint2*>(kc);
-        r.k[i][0] = w.x; r.k[i][1] = w.y;
-        r.ks[i] = ks[g >> 1];
+        const uint2 w = *reinterpret_cast<const uint2*>(kc + k_at);
+        k[i][0] = w.x; k[i][1] = w.y;
       } else {
 #pragma unroll
         for (int x = 0; x < D / 128; ++x) {
-          const uint4 w = reinterpret_cast<const uint4*>(kc)[x];
-          r.k[i][4 * x] = w.x; r.k[i][4 * x + 1] = w.y; r.k[i][4 * x + 2] = w.z; r.k[i][4 * x + 3] = w.w;
+          const uint4 w = *reinterpret_cast<const uint4*>(kc + k_at + 16 * x);
+          k[i][4 * x] = w.x; k[i][4 * x + 1] = w.y; k[i][4 * x + 2] = w.z; k[i][4 * x + 3] = w.w;
         }
-        if constexpr (D == 128) r.ks[i] = ks[g];
-        else r.ks[i] = *reinterpret_cast<const uint16_t*>(ks + 2 * g);
       }
+      ks[i] = D == 256 ? *reinterpret_cast<const uint16_t*>(sc + ks_at) : sc[ks_at];
+      if (gr[i].bad) ks[i] = 0xffffu;
+    }
+  };
+  auto load_v = [&]() {                                                  // of the step load_k was last called for
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint8_t* vc = p.c.vc + gr[i].base * (D / 2);
+      const uint8_t* sc = p.c.vs + gr[i].base * (D / 32);
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-        const int eighth = (n & (D / 8 - 1)) + 16 * c;                  // D = 64: lanes n and n + 8 share a piece
-        r.v[i][c] = *reinterpret_cast<const uint4*>(vc + (g * (D / 8) + eighth) * 16);
-        r.vs[i][c] = *reinterpret_cast<const uint32_t*>(vs + (g * (D / 32) + eighth / 4) * 4);
-      }
-      if (bad) {
-        r.ks[i] = 0xffffu;
-#pragma unroll
-        for (int c = 0; c < NC; ++c) r.vs[i][c] = 0xffffffffu;
+        v[i][c] = *reinterpret_cast<const uint4*>(vc + v_at[c]);
+        vs[i][c] = *reinterpret_cast<const uint32_t*>(sc + vs_at[c]);
+        if (gr[i].bad) vs[i][c] = 0xffffffffu;
       }
     }
   };
 
-  for (int step = wave; step < steps; step += kWaves) {
-    Raw<D> r;
-    load(step, r);
-    const int at = t0 + step * kUnit;
+  look_up(s0);
+  load_k(s0);
+  load_v();
+  for (int s = s0; s < s1; ++s) {
+    const int at = t.lo + s * kUnit;
     // scores of the lane's row against tokens at + 16 i + 4 g + j
-    f32x4 s[2];
+    f32x4 x[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      s[i] = f32x4{0, 0, 0, 0};
+      x[i] = f32x4{0, 0, 0, 0};
 #pragma unroll
-      for (int x = 0; x < KS; ++x) {
-        const float unit = unit_of(r.ks[i], D == 256 ? x / 4 : 0);
-        const bf16x8 a = frag(fp4_pair(r.k[i][x], unit, 0), fp4_pair(r.k[i][x], unit, 1),
-                              fp4_pair(r.k[i][x], unit, 2), fp4_pair(r.k[i][x], unit, 3));
+      for (int y = 0; y < KS; ++y) {
+        const float unit = unit_of(ks[i], D == 256 ? y / 4 : 0);
+        const bf16x8 a = frag(fp4_pair(k[i][y], unit, 0), fp4_pair(k[i][y], unit, 1),
+                              fp4_pair(k[i][y], unit, 2), fp4_pair(k[i][y], unit, 3));
 #pragma unroll
-        for (int y = 0; y < NS; ++y) s[i] = mfma(a, qf[x][y], s[i]);
+        for (int z = 0; z < NS; ++z) x[i] = mfma(a, qf[y][z], x[i]);
       }
     }
+    // the next keys are on their way during the softmax and the second product,
+    // the next values during the next first product (past the end: the last step's again)
+    const int next = min(s + 1, s1 - 1);
+    if (((next - s0) & 31) == 0 && next != s0) look_up(next);
+    load_k(next);
+
     float sc[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sc[i] = s[i >> 2][i & 3] * p.scale_log2e;
-    const bool masked = at + kUnit > min(all_hi, t1) || at < all_lo;    // the same for the whole wave
-    bool nan_value[NC] = {};
-    float gone[8];                                                       // weights of the values that are NaN
+    for (int i = 0; i < 8; ++i) sc[i] = x[i >> 2][i & 3] * p.scale_log2e;
+    const bool masked = at + kUnit > all_hi || at < all_lo;              // the same for the whole wave
     if (masked) {
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int tok = at + 16 * i + 4 * g + j;
-          const bool seen = tok <= pos && tok >= first && tok < t1;
-          if (!seen) sc[4 * i + j] = -INFINITY;
-          gone[4 * i + j] = seen ? 1.0f : 0.0f;
-        }
-      // A weight of zero does not hide a NaN value: NaN blocks are taken out of
-      // the product, and the rows that do see one are made NaN below.
-#pragma unroll
-      for (int c = 0; c < NC; ++c)
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            nan_value[c] |= ((r.vs[i][c] >> (8 * j)) & 0xffu) == 0xffu;
+        for (int j = 0; j < 4; ++j)
+          if (!seen(at, i, j)) sc[4 * i + j] = -INFINITY;
     }
     float top = sc[0];
 #pragma unroll
     for (int i = 1; i < 8; ++i) top = fmaxf(top, sc[i]);
-    const float m_new = fmaxf(m, max_over_groups(top));
+    const float m_new = fmaxf(st.m, max_over_groups(top));
     const float base = m_new == -INFINITY ? 0.0f : m_new;
-    const float fade = __builtin_amdgcn_exp2f(m - base);
-    m = m_new;
+    if (__any(m_new > st.m)) {                                           // seldom after the first steps
+      const float fade = __builtin_amdgcn_exp2f(st.m - base);
+      st.l *= fade;
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int e = 0; e < NB; ++e) st.o[c][e] *= fade;
+      st.m = m_new;
+    }
     float w[8];
-    l *= fade;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       w[i] = __builtin_amdgcn_exp2f(sc[i] - base);
-      l += w[i];
+      st.l += w[i];
     }
-#pragma unroll
-    for (int c = 0; c < NC; ++c)
-#pragma unroll
-      for (int e = 0; e < NB; ++e) o[c][e] *= fade;
     bf16x8 pf[NS];
     split<NS>(w, pf);
 
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-      if (masked && __any(nan_value[c])) {
-        uint32_t hit[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) hit[i] = 0;
+      if (masked) {
+        // A weight of zero does not hide a NaN value: NaN blocks are taken out of
+        // the product, and the rows that do see one are made NaN.
+        uint32_t hit[4] = {0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            if (((r.vs[i][c] >> (8 * j)) & 0xffu) == 0xffu) {
-              hit[2 * i + j / 2] |= 0x3f80u << (16 * (j & 1));
-              r.vs[i][c] ^= 0x80u << (8 * j);                            // 255 -> 127
-              (&r.v[i][c].x)[j] = 0;
+            if (((vs[i][c] >> (8 * j)) & 0xffu) == 0xffu) hit[2 * i + j / 2] |= 0x3f80u << (16 * (j & 1));
+        if (__any((hit[0] | hit[1] | hit[2] | hit[3]) != 0)) {
+          float in[8];
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              in[4 * i + j] = seen(at, i, j) ? 1.0f : 0.0f;
+              if (((vs[i][c] >> (8 * j)) & 0xffu) == 0xffu) {
+                vs[i][c] ^= 0x80u << (8 * j);                            // 255 -> 127
+                (&v[i][c].x)[j] = 0;
+              }
             }
-        bf16x8 seen[1];
-        split<1>(gone, seen);
-        const f32x4 count = mfma(frag(hit[0], hit[1], hit[2], hit[3]), seen[0], f32x4{0, 0, 0, 0});
+          bf16x8 who[1];
+          split<1>(in, who);
+          const f32x4 count = mfma(frag(hit[0], hit[1], hit[2], hit[3]), who[0], f32x4{0, 0, 0, 0});
 #pragma unroll
-        for (int e = 0; e < NB; ++e)
+          for (int e = 0; e < NB; ++e)
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (count[i] > 0.0f) o[c][e][i] = NAN;
-      }
-      const uint32_t* vw[2] = {&r.v[0][c].x, &r.v[1][c].x};
-      uint32_t word[2][4];
-      float unit[2][4];
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          word[i][j] = D == 64 ? vw[i][j] >> (16 * (n >> 3)) : vw[i][j];
-          unit[i][j] = unit_of(r.vs[i][c], j);
+            for (int i = 0; i < 4; ++i)
+              if (count[i] > 0.0f) st.o[c][e][i] = NAN;
         }
+      }
+      const uint32_t* vw[2] = {&v[0][c].x, &v[1][c].x};
 #pragma unroll
       for (int e = 0; e < NB / 2; ++e) {
-        uint32_t x[2][4];
+        uint32_t y[2][4];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) x[i][j] = fp4_pair(word[i][j], unit[i][j], e);
-        const bf16x8 even = frag(__builtin_amdgcn_perm(x[0][1], x[0][0], 0x05040100u), __builtin_amdgcn_perm(x[0][3], x[0][2], 0x05040100u),
-                                 __builtin_amdgcn_perm(x[1][1], x[1][0], 0x05040100u), __builtin_amdgcn_perm(x[1][3], x[1][2], 0x05040100u));
-        const bf16x8 odd = frag(__builtin_amdgcn_perm(x[0][1], x[0][0], 0x07060302u), __builtin_amdgcn_perm(x[0][3], x[0][2], 0x07060302u),
-                                __builtin_amdgcn_perm(x[1][1], x[1][0], 0x07060302u), __builtin_amdgcn_perm(x[1][3], x[1][2], 0x07060302u));
+          for (int j = 0; j < 4; ++j)
+            y[i][j] = fp4_pair(D == 64 ? vw[i][j] >> (16 * (n >> 3)) : vw[i][j], unit_of(vs[i][c], j), e);
+        const bf16x8 even = frag(__builtin_amdgcn_perm(y[0][1], y[0][0], 0x05040100u), __builtin_amdgcn_perm(y[0][3], y[0][2], 0x05040100u),
+                                 __builtin_amdgcn_perm(y[1][1], y[1][0], 0x05040100u), __builtin_amdgcn_perm(y[1][3], y[1][2], 0x05040100u));
+        const bf16x8 odd = frag(__builtin_amdgcn_perm(y[0][1], y[0][0], 0x07060302u), __builtin_amdgcn_perm(y[0][3], y[0][2], 0x07060302u),
+                                __builtin_amdgcn_perm(y[1][1], y[1][0], 0x07060302u), __builtin_amdgcn_perm(y[1][3], y[1][2], 0x07060302u));
 #pragma unroll
-        for (int y = 0; y < NS; ++y) {
-          o[c][2 * e] = mfma(even, pf[y], o[c][2 * e]);
-          o[c][2 * e + 1] = mfma(odd, pf[y], o[c][2 * e + 1]);
+        for (int z = 0; z < NS; ++z) {
+          st.o[c][2 * e] = mfma(even, pf[z], st.o[c][2 * e]);
+          st.o[c][2 * e + 1] = mfma(odd, pf[z], st.o[c][2 * e + 1]);
         }
       }
     }
+    load_v();
   }
+  st.l = sum_over_groups(st.l);
+}
 
-  // join the waves: result row 4 g + i of piece c is elements 8 (4 g + i + 16 c) + e (D = 64: 8 of (4 g + i) % 8, half each)
-  l = sum_over_groups(l);
-#pragma unroll
-  for (int c = 0; c < NC; ++c)
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int e = 0; e < NB; e += 4) {
-        const int r = 4 * g + i;
-        const int at = D == 64 ? 8 * (r & 7) + 4 * (r >> 3) + e : 8 * (r + 16 * c) + e;
-        *reinterpret_cast<float4*>(&lds_o[wave][n][at]) = make_float4(o[c][e][i], o[c][e + 1][i], o[c][e + 2][i], o[c][e + 3][i]);
-      }
-  if (g == 0) { lds_m[wave][n] = m; lds_l[wave][n] = l; }
-  __syncthreads();
+// A query row's address in out.
+template <int D, typename TQ>
+__device__ __forceinline__ TQ* out_at(const AttnParams& p, const Tile& t, int h, int r) {
+  const int row = t.row0 + r, query = row / p.group;
+  return static_cast<TQ*>(p.out) + (t.q0 + query) * p.ldo + static_cast<int64_t>(h * p.group + row - query * p.group) * D;
+}
 
-  const int64_t tile = (static_cast<int64_t>(b) * p.subs + sub) * p.c.heads + h;
-  const int n_rows = min(kRowTile, t.rows - t.row0);
-  float* const ml = p.part + static_cast<int64_t>(p.B) * p.subs * p.c.heads * p.pieces * p.part_rows * D;
-  for (int k = threadIdx.x; k < n_rows * (D / 8); k += kThreads) {
-    const int r = k / (D / 8), e = (k % (D / 8)) * 8;
-    float M = -INFINITY;
+// The batch's steps (of the sequences with few rows), tile after tile and head
+// after head, are dealt out to the waves in equal runs, however the lengths
+// differ.  A run starts and ends inside a tile as a rule: those two leave their
+// sums in the workspace (slots 2 w and 2 w + 1) for the join, the tiles between
+// are whole and final.
+template <int D, typename TQ>
+__global__ __launch_bounds__(256, D == 256 || sizeof(TQ) == 4 ? 2 : 4) void attn_runs_kernel(AttnParams p) {
+  constexpr int NC = State<D>::NC, NB = State<D>::NB;
+  const int lane = threadIdx.x & 63, tiles = p.B * p.subs;
+  const int w = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+  int4* const info = reinterpret_cast<int4*>(p.info);
+  int mine = 0;
+  for (int i = lane; i < tiles; i += 64) {
+    const int steps = small_tile(p, i).steps;
+    if (steps == 0 && i % p.runs == w)
+      for (int h = 0; h < p.c.heads; ++h) info[static_cast<int64_t>(i) * p.c.heads + h] = make_int4(0, 0, 0, 0);
+    mine += steps;
+  }
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, lds_m[w][r]);
-    const float base = M == -INFINITY ? 0.0f : M;
-    float L = 0.0f, f[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  for (int k = 1; k < 64; k <<= 1) mine += __shfl_xor(mine, k);
+  const int total = __builtin_amdgcn_readfirstlane(mine) * p.c.heads;
+  if (total == 0) return;
+  // a run of kMinRun steps at least; the first `more` runs are one longer
+  const int runs = min(p.runs, (total + kMinRun - 1) / kMinRun);
+  if (w >= runs) return;
+  const int len = total / runs, more = total - len * runs;
+  const int u0 = w * len + min(w, more), u1 = u0 + len + (w < more ? 1 : 0);
+  // the tile that holds step u0, and that tile's first step
+  int index = 0, start = 0;
+  for (int base = 0, before = 0; base < tiles; base += 64) {
+    const int n = base + lane < tiles ? small_tile(p, base + lane).steps * p.c.heads : 0;
+    int to = n;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const float a = __builtin_amdgcn_exp2f(lds_m[w][r] - base);
-      L += a * lds_l[w][r];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) f[i] += a * lds_o[w][r][e + i];
+    for (int k = 1; k < 64; k <<= 1) {
+      const int up = __shfl_up(to, k);
+      if (lane >= k) to += up;
     }
-    if (n_pieces == 1) {
-      const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+    const uint64_t here = __ballot(before + to > u0);                   // the first such lane's tile
+    if (here) {
+      const int first = __builtin_ctzll(here);
+      index = base + first;
+      start = before + __builtin_amdgcn_readlane(to - n, first);
+      break;
+    }
+    before += __builtin_amdgcn_readlane(to, 63);
+  }
+  Tile t = uniform(small_tile(p, index));
+  int h = (u0 - start) / t.steps, step = u0 - start - h * t.steps;
+  const int n = lane & 15, g = lane >> 4;
+  for (int u = u0; u < u1;) {
+    const int steps = min(t.steps - step, u1 - u);
+    State<D> st;
+    attend<D, TQ>(p, t, h, step, step + steps, st);
+    const bool whole = steps == t.steps;
+    const int slot = 2 * w + (u == u0 ? 0 : 1);
+    if (t.row0 + n < t.rows) {
+      if (whole) {
+        const float inv = st.l == 0.0f ? 0.0f : 1.0f / st.l;
+        TQ* const o = out_at<D, TQ>(p, t, h, n);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) f[i] *= inv;
-      const int q_row = t.row0 + r;
-      store_out(static_cast<TQ*>(p.out) + (t.q0 + q_row / p.group) * p.ldo +
-                    static_cast<int64_t>(h * p.group + q_row % p.group) * D + e, f);
-    } else {
-      const int64_t at = (tile * p.pieces + piece) * p.part_rows + r;
-      float4* o4 = reinterpret_cast<float4*>(p.part + at * D + e);
-      o4[0] = make_float4(f[0], f[1], f[2], f[3]);
-      o4[1] = make_float4(f[4], f[5], f[6], f[7]);
-      if (e == 0) { ml[2 * at] = M; ml[2 * at + 1] = L; }
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float f[NB];
+#pragma unroll
+            for (int e = 0; e < NB; ++e) f[e] = st.o[c][e][i] * inv;
+            store_out<NB>(o + State<D>::element(g, c, i), f);
+          }
+      } else {
+        const int64_t at = static_cast<int64_t>(slot) * p.part_rows + n;
+        float* const o = p.part + at * D;
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float f[NB];
+#pragma unroll
+            for (int e = 0; e < NB; ++e) f[e] = st.o[c][e][i];
+            store_out<NB>(o + State<D>::element(g, c, i), f);
+          }
+        if (g == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * at) = make_float2(st.m, st.l);
+      }
+    }
+    if (step == 0 && lane == 0) {
+      // the tile starts here; its pieces end in the run that holds its last step
+      const int last = u + t.steps - 1, cut = (len + 1) * more;
+      const int to = last < cut ? last / (len + 1) : more + (last - cut) / len;
+      info[static_cast<int64_t>(index) * p.c.heads + h] = make_int4(to - w + 1, slot, t.q0, t.row0 << 8 | min(kRowTile, t.rows - t.row0));
+    }
+    u += steps;
+    step = 0;
+    if (u < u1 && ++h == p.c.heads) {
+      h = 0;
+      do t = uniform(small_tile(p, ++index)); while (t.steps == 0);
     }
   }
 }
 
-// Joins a tile's pieces, in their order.
+// Joins the pieces of tile blockIdx.x (tile x head), row blockIdx.y, in their order:
+// threads take four elements of every kJoin-th piece.  All that it has to know of
+// the tile stands in its info: two trips to memory, not a chain of look-ups.
 template <int D, typename TQ>
-__global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnParams p) {
-  int id = blockIdx.x;
-  const int h = id % p.c.heads; id /= p.c.heads;
-  const int sub = id % p.subs, b = id / p.subs;
+__global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(AttnParams p) {
+  constexpr int kJoin = kJoinThreads / (D / 4);
+  __shared__ float4 part[kJoin][D / 4];
+  __shared__ float len[kJoin];
+  const int4 info = reinterpret_cast<const int4*>(p.info)[blockIdx.x];
+  const int h = blockIdx.x % p.c.heads, r = blockIdx.y;
+  const int n = info.x;
+  if (n < 2 || r >= (info.w & 255)) return;
+  const int first = info.y, w = first >> 1;
+  auto row_of = [&](int k) { return static_cast<int64_t>(k ? 2 * (w + k) : first) * p.part_rows + r; };
+  const int e = threadIdx.x % (D / 4), group = threadIdx.x / (D / 4);
+  float M = -INFINITY;
+  for (int k = threadIdx.x & 63; k < n; k += 64) M = fmaxf(M, p.part_ml[2 * row_of(k)]);
+#pragma unroll
+  for (int k = 1; k < 64; k <<= 1) M = fmaxf(M, __shfl_xor(M, k));
+  const float base = M == -INFINITY ? 0.0f : M;
+  float L = 0.0f;
+  float4 f = make_float4(0, 0, 0, 0);
+#pragma unroll 4
+  for (int k = group; k < n; k += kJoin) {
+    const int64_t at = row_of(k);
+    const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + 2 * at);
+    const float4 x = *reinterpret_cast<const float4*>(p.part + at * D + 4 * e);
+    const float a = __builtin_amdgcn_exp2f(ml.x - base);
+    L += a * ml.y;
+    f.x += a * x.x; f.y += a * x.y; f.z += a * x.z; f.w += a * x.w;
+  }
+  part[group][e] = f;
+  if (e == 0) len[group] = L;
+  __syncthreads();
+  if (threadIdx.x >= D / 8) return;
+  L = 0.0f;
+  float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+  for (int k = 0; k < kJoin; ++k) {
+    L += len[k];
+    const float4 x = part[k][2 * threadIdx.x], y = part[k][2 * threadIdx.x + 1];
+    s[0] += x.x; s[1] += x.y; s[2] += x.z; s[3] += x.w;
+    s[4] += y.x; s[5] += y.y; s[6] += y.z; s[7] += y.w;
+  }
+  const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) s[i] *= inv;
   Tile t;
-  if (!tile_of(p, b, sub, &t)) return;
-  const int n_pieces = pieces_of(p, t);
-  if (n_pieces == 1) return;
-  const int64_t tile = blockIdx.x;
-  const int n_rows = min(kRowTile, t.rows - t.row0);
-  const float* const ml = p.part + static_cast<int64_t>(p.B) * p.subs * p.c.heads * p.pieces * p.part_rows * D;
-  for (int k = threadIdx.x; k < n_rows * (D / 8); k += kThreads) {
+  t.q0 = info.z;
+  t.row0 = info.w >> 8;
+  store_out<8>(out_at<D, TQ>(p, t, h, r) + 8 * threadIdx.x, s);
+}
+
+// A workgroup takes a whole tile, its WAVES waves a share of its steps each, and
+// joins them in shared memory.  large: the tiles of the sequences with many rows,
+// found by counting them (their number is known on the device only).
+template <int D, typename TQ, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void attn_tile_kernel(AttnParams p, int large) {
+  constexpr int NC = State<D>::NC, NB = State<D>::NB;
+  extern __shared__ float lds[];                   // [WAVES][part_rows][D + 4], then [WAVES][part_rows][2]
+  float* const ml = lds + WAVES * p.part_rows * (D + 4);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int index = blockIdx.x / p.c.heads, h = blockIdx.x - index * p.c.heads;
+  Tile t;
+  if (large) {
+    int b = -1, sub = 0;
+    for (int base = 0, before = 0; base < p.B && b < 0; base += 64) {
+      int n = 0;
+      if (base + lane < p.B) {
+        const int rows = min(queries_of(p, base + lane).n, p.max_q) * p.group;
+        n = rows > kSmallRows ? (rows + kRowTile - 1) / kRowTile : 0;
+      }
+      int to = n;
+#pragma unroll
+      for (int k = 1; k < 64; k <<= 1) {
+        const int up = __shfl_up(to, k);
+        if (lane >= k) to += up;
+      }
+      const uint64_t here = __ballot(before + to > index);
+      if (here) {
+        const int at = __builtin_ctzll(here);
+        b = base + at;
+        sub = index - before - __builtin_amdgcn_readlane(to - n, at);
+      }
+      before += __builtin_amdgcn_readlane(to, 63);
+    }
+    if (b < 0) return;
+    t = uniform(tile_of(p, b, sub));
+  } else {
+    t = uniform(small_tile(p, index));
+  }
+  if (t.steps == 0) return;
+  const int s0 = t.steps * wave / WAVES, s1 = t.steps * (wave + 1) / WAVES;
+  const int n = lane & 15, g = lane >> 4;
+  if (s0 < s1) {
+    State<D> st;
+    attend<D, TQ>(p, t, h, s0, s1, st);
+    if (t.row0 + n < t.rows) {
+      float* const o = lds + (wave * p.part_rows + n) * (D + 4);
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float f[NB];
+#pragma unroll
+          for (int e = 0; e < NB; ++e) f[e] = st.o[c][e][i];
+          store_out<NB>(o + State<D>::element(g, c, i), f);
+        }
+      if (g == 0) *reinterpret_cast<float2*>(ml + 2 * (wave * p.part_rows + n)) = make_float2(st.m, st.l);
+    }
+  } else if (lane < p.part_rows) {                 // fewer steps than waves
+    *reinterpret_cast<float2*>(ml + 2 * (wave * p.part_rows + lane)) = make_float2(-INFINITY, 0.0f);
+  }
+  __syncthreads();
+  const int rows = min(kRowTile, t.rows - t.row0);
+  for (int k = threadIdx.x; k < rows * (D / 8); k += 64 * WAVES) {
     const int r = k / (D / 8), e = (k % (D / 8)) * 8;
     float M = -INFINITY;
-    for (int s = 0; s < n_pieces; ++s) M = fmaxf(M, ml[2 * ((tile * p.pieces + s) * p.part_rows + r)]);
+#pragma unroll
+    for (int v = 0; v < WAVES; ++v) M = fmaxf(M, ml[2 * (v * p.part_rows + r)]);
     const float base = M == -INFINITY ? 0.0f : M;
     float L = 0.0f, f[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    for (int s = 0; s < n_pieces; ++s) {
-      const int64_t at = (tile * p.pieces + s) * p.part_rows + r;
-      const float a = __builtin_amdgcn_exp2f(ml[2 * at] - base);
-      L += a * ml[2 * at + 1];
-      const float4* o4 = reinterpret_cast<const float4*>(p.part + at * D + e);
-      const float4 x = o4[0], y = o4[1];
+#pragma unroll
+    for (int v = 0; v < WAVES; ++v) {
+      const float2 w = *reinterpret_cast<const float2*>(ml + 2 * (v * p.part_rows + r));
+      if (w.y == 0.0f) continue;                   // saw nothing: no sums
+      const float a = __builtin_amdgcn_exp2f(w.x - base);
+      L += a * w.y;
+      const float4* o = reinterpret_cast<const float4*>(lds + (v * p.part_rows + r) * (D + 4) + e);
+      const float4 x = o[0], y = o[1];
       f[0] += a * x.x; f[1] += a * x.y; f[2] += a * x.z; f[3] += a * x.w;
       f[4] += a * y.x; f[5] += a * y.y; f[6] += a * y.z; f[7] += a * y.w;
     }
     const float inv = L == 0.0f ? 0.0f : 1.0f / L;
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] *= inv;
-    const int q_row = t.row0 + r;
-    store_out(static_cast<TQ*>(p.out) + (t.q0 + q_row / p.group) * p.ldo +
-                  static_cast<int64_t>(h * p.group + q_row % p.group) * D + e, f);
+    store_out<8>(out_at<D, TQ>(p, t, h, r) + e, f);
   }
 }
 
+template <int D, typename TQ, int WAVES>
+void launch_tiles(const AttnParams& p, int64_t tiles, int large, hipStream_t s) {
+  const size_t lds = static_cast<size_t>(WAVES) * p.part_rows * (D + 6) * sizeof(float);
+  attn_tile_kernel<D, TQ, WAVES><<<static_cast<uint32_t>(tiles * p.c.heads), 64 * WAVES, lds, s>>>(p, large);
+}
+
 template <int D, typename TQ> hipError_t launch(const AttnParams& p, hipStream_t s) {
-  const uint32_t tiles = static_cast<uint32_t>(static_cast<int64_t>(p.B) * p.subs * p.c.heads);
-  attn_rows_kernel<D, TQ><<<tiles * p.pieces, kThreads, 0, s>>>(p);
-  if (p.pieces > 1) attn_join_kernel<D, TQ><<<tiles, kThreads, 0, s>>>(p);
+  const int64_t small = static_cast<int64_t>(p.B) * p.subs;
+  if (p.whole) {
+    if (p.whole == 8) launch_tiles<D, TQ, 8>(p, small, 0, s);
+    else launch_tiles<D, TQ, 2>(p, small, 0, s);
+  } else {
+    attn_runs_kernel<D, TQ><<<(p.runs + 3) / 4, 256, 0, s>>>(p);
+    attn_join_kernel<D, TQ><<<dim3(static_cast<uint32_t>(small * p.c.heads), p.part_rows), kJoinThreads, 0, s>>>(p);
+  }
+  if (static_cast<int64_t>(p.max_q) * p.group > kSmallRows)
+    launch_tiles<D, TQ, D == 256 ? 2 : 4>(p, p.large_tiles, 1, s);
   return hipGetLastError();
 }
 
-// Workgroups that a long axis is split up to: a few for every compute unit.
-constexpr int64_t kTargetGroups = 1024;
-constexpr int kChunkUnit = kUnit * kWaves;
-
 }  // namespace
 
-size_t plan_attention(AttnParams* p) {
-  p->subs = static_cast<int>((static_cast<int64_t>(p->max_q) * p->group + kRowTile - 1) / kRowTile);
-  const int64_t tiles = static_cast<int64_t>(p->B) * p->subs * p->c.heads;
+bool plan_attention(AttnParams* p, size_t* bytes) {
+  const int64_t rows = static_cast<int64_t>(p->max_q) * p->group;
+  p->subs = static_cast<int>((std::min<int64_t>(rows, kSmallRows) + kRowTile - 1) / kRowTile);
+  p->part_rows = static_cast<int>(std::min<int64_t>(kRowTile, rows));
+  // tiles of sequences with more rows than the small ones have
+  p->large_tiles = (static_cast<int64_t>(p->T) * p->group + kRowTile - 1) / kRowTile +
+                   std::min<int64_t>(p->B, static_cast<int64_t>(p->T) * p->group / kSmallRows);
   // a window's span: the tile's queries, and its start rounded down to a step
   int64_t span = p->max_kv;
   if (p->window) span = std::min<int64_t>(span, static_cast<int64_t>(p->window) + kRowTile + kUnit);
-  span = std::max<int64_t>(span, 1);
-  const int64_t most = (span + kChunkUnit - 1) / kChunkUnit;
-  const int64_t per = (span * std::max<int64_t>(tiles, 1) + kTargetGroups - 1) / kTargetGroups;
-  const int64_t chunk = std::min(most, (per + kChunkUnit - 1) / kChunkUnit) * kChunkUnit;
-  p->chunk = static_cast<int>(chunk);
-  p->pieces = static_cast<int>((span + chunk - 1) / chunk);
-  p->part_rows = static_cast<int>(std::min<int64_t>(kRowTile, static_cast<int64_t>(p->max_q) * p->group));
-  // tiles x pieces is at most tiles x most and less than the target and one a tile more
-  const uint64_t parts = std::min(tiles * most, kTargetGroups + tiles);
-  return 256 + parts * p->part_rows * (p->c.d + 2) * sizeof(float);
+  const int64_t tiles = static_cast<int64_t>(p->B) * p->subs * p->c.heads;
+  if (tiles > 0x7fffffff || p->large_tiles * p->c.heads > 0x7fffffff) return false;
+  const int64_t steps = tiles * std::max<int64_t>(1, (span + kUnit - 1) / kUnit);
+  if (steps > 0x7fffffff) return false;
+  // A tile's steps shared by one workgroup's waves need no join, but last as long as the
+  // longest sequence does.  Measured at 32 + 8 heads of 128, whole tiles against runs:
+  // 1 request of 1024 tokens 8.7 / 10.5 us, of 2048 12.7 / 10.9, of 8192 36 / 14; 8 of 4096
+  // 23 / 20; 64 of 4096 60 / 72, of 8192 108 / 121 (of 1000 to 8192 76 / 84).
+  p->whole = span <= 2048 || (span <= 8192 && tiles >= 192) ? 8 : 0;
+  if (p->whole && static_cast<int64_t>(p->part_rows) * (p->c.d + 6) * 32 > 65536) p->whole = 2;
+  p->runs = static_cast<int>(std::min<int64_t>(kRuns, (steps + kMinRun - 1) / kMinRun));
+  // sums of two slots a run, their maxima and lengths, four numbers a tile
+  const size_t slots = static_cast<size_t>(2) * p->runs * p->part_rows;
+  *bytes = slots * (p->c.d + 2) * sizeof(float) + static_cast<size_t>(tiles) * 16;
+  return true;
+}
+
+void place_attention(AttnParams* p, void* workspace) {
+  const int64_t slots = static_cast<int64_t>(2) * p->runs * p->part_rows;
+  p->part = static_cast<float*>(workspace);
+  p->part_ml = p->part + slots * p->c.d;
+  p->info = reinterpret_cast<int32_t*>(p->part_ml + slots * 2);
 }
 
 hipError_t launch_attention(const AttnParams& p, hipStream_t s) {

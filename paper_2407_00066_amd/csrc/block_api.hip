@@ -103,11 +103,10 @@ int plan(const cts_attn_problem* p, const cts_kv_cache* c, cts::AttnParams* a, s
   const int64_t room = static_cast<int64_t>(p->max_pages) << shift;
   a->max_kv = static_cast<int>(std::min<int64_t>(p->max_kv, room));
   a->scale_log2e = p->scale * 1.4426950408889634f;
-  const unsigned __int128 tiles = (static_cast<uint64_t>(p->max_q) * a->group + 15) / 16;
-  if (tiles * p->B * c->n_heads > kMaxGrid / 64)
+  // (bounds that keep the plan's own arithmetic in 64 bits)
+  if (static_cast<uint64_t>(p->B) * c->n_heads > kMaxGrid || static_cast<uint64_t>(p->T) * p->n_q_heads > kMaxGrid)
     return CTS_ERR_UNSUPPORTED;
-  *bytes = cts::plan_attention(a);
-  return CTS_OK;
+  return cts::plan_attention(a, bytes) ? CTS_OK : CTS_ERR_UNSUPPORTED;
 }
 
 }  // namespace
@@ -173,7 +172,7 @@ int cts_kv_attention(const cts_attn_problem* p, const cts_kv_cache* c, const voi
   if (workspace_bytes < need) return CTS_ERR_WORKSPACE;
   a.q = q; a.ldq = ldq; a.out = out; a.ldo = ldo;
   a.table = block_table; a.kv_len = kv_len; a.q_start = q_start;
-  a.part = static_cast<float*>(workspace);
+  cts::place_attention(&a, workspace);
   return status(cts::launch_attention(a, static_cast<hipStream_t>(stream)));
 }
 

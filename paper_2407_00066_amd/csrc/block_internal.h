@@ -29,15 +29,20 @@ struct AttnParams {
   int T, B, heads, group;           // group: query heads of a key/value head
   int max_pages, max_q, max_kv, window, dtype;
   float scale_log2e;
-  // the plan: 16-row tiles of a sequence, tokens of a piece, pieces
-  int subs, chunk, pieces;
-  int part_rows;                    // rows of a tile that partials are kept for
-  float* part;                      // [B][subs][kv heads][pieces][part_rows][d], then [..][part_rows][2]
+  // the plan: 16-row tiles of a sequence with few rows, waves its steps are dealt
+  // out to, rows of a tile that sums are kept for, tiles of the other sequences
+  int subs, runs, part_rows;
+  int whole;                        // waves of a workgroup that takes a whole tile; 0: runs
+  int64_t large_tiles;
+  float *part, *part_ml;            // [2 runs][part_rows][d] sums, [2 runs][part_rows][2] maxima and lengths
+  int32_t* info;                    // [tiles][kv heads][4] a tile's pieces, the first one's slot, its query row, first row and rows
 };
 
-// Chooses subs, chunk, pieces and part_rows, and gives the workspace's bytes
-// (not falling with any size).
-size_t plan_attention(AttnParams* p);
+// Chooses the plan and gives the workspace's bytes (not falling with any size);
+// false for a batch whose steps or workgroups 31 bits do not count.
+bool plan_attention(AttnParams* p, size_t* bytes);
+// Lays the workspace out for the plan.
+void place_attention(AttnParams* p, void* workspace);
 hipError_t launch_attention(const AttnParams& p, hipStream_t s);
 
 struct NormParams {
