@@ -1,0 +1,329 @@
+// Attention over the 4-bit cache for sequences with many query rows (prompts and
+// chunks of prompts), bf16: the same one-pass softmax and the same transposed
+// products as attention.hip, on 32 x 32 tiles.
+//
+// A workgroup's waves take 32 query rows each (query x head of one key/value
+// head's group, in that order) and walk the visible tokens together, 8192 / D of
+// them a step.  A step's codes become bf16 once for the whole workgroup, in
+// shared memory: keys as they lie, [token][element]; values turned, [element][token],
+// their tokens in the order in which the first product's result leaves them in
+// the lanes, so that the weights are the second product's operand as they stand.
+// Rows are rotated in 16-byte pieces so that neither side meets a bank twice.
+// One buffer is filled while the other is multiplied: a barrier a step.
+//
+// Lane l = 32 hh + n.  First product: A row = token n of 32, k = elements 16 s + 8 hh
+// .. + 7 in step s; result: register i is token 8 (i / 4) + 4 hh + i % 4, column n =
+// query row.  Second: A row = element n of 32, k = 8 hh + j for the tokens
+// 8 (j / 4) + 4 hh + j % 4 of 16.
+#include <algorithm>
+
+#include "attention_common.h"
+
+namespace cts {
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+__device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+
+template <int D> struct Step {
+  static constexpr int T = 8192 / D;               // tokens
+  static constexpr int MB = T / 32;                // row blocks of the first product
+  static constexpr int DB = D / 32;                // row blocks of the second; scale blocks
+  static constexpr int KS = D / 16;                // k steps of the first
+  static constexpr int KC = D / 8, VC = T / 8;     // 16-byte pieces of a row of keys, of values
+  static __device__ __forceinline__ int key(int tok, int c) { return (tok * KC + (c ^ (tok & (KC < 16 ? KC - 1 : 15)))) * 16; }
+  static __device__ __forceinline__ int value(int d, int c) {
+    return (d * VC + (c ^ (VC == 4 ? (d >> 1) & 3 : d & (VC - 1)))) * 16;
+  }
+};
+
+template <int D> struct TileShared {
+  char k[2][8192 * 2], v[2][8192 * 2];
+  uint64_t nan[3][(Step<D>::T + 63) / 64][Step<D>::DB];                  // tokens whose value block is NaN
+};
+
+template <int D, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attn_prompt_kernel(AttnParams p) {
+  using S = Step<D>;
+  constexpr int ROWS = 32 * WAVES;
+  constexpr bool kBoth = WAVES == 4;               // 512 threads: half of them convert keys, half values; 256: all both
+  __shared__ TileShared<D> sh;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 31, hh = lane >> 5;
+  const int index = blockIdx.x / p.c.heads, h = blockIdx.x - index * p.c.heads;
+  int b = -1, sub = 0;
+  for (int base = 0, before = 0; base < p.B && b < 0; base += 64) {
+    int count = 0;
+    if (base + lane < p.B) {
+      const int rows = min(queries_of(p, base + lane).n, p.max_q) * p.group;
+      count = rows > kSmallRows ? (rows + ROWS - 1) / ROWS : 0;
+    }
+    int to = count;
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) {
+      const int up = __shfl_up(to, k);
+      if (lane >= k) to += up;
+    }
+    const uint64_t here = __ballot(before + to > index);
+    if (here) {
+      const int at = __builtin_ctzll(here);
+      b = base + at;
+      // a sequence's last rows see most: they go first
+      sub = before + __builtin_amdgcn_readlane(to, at) - 1 - index;
+    }
+    before += __builtin_amdgcn_readlane(to, 63);
+  }
+  if (b < 0) return;
+  const Queries q = queries_of(p, b);
+  const int len = min(max(p.kv_len[b], 0), p.max_kv);
+  const int rows = min(q.n, p.max_q) * p.group, first_pos = len - q.n;
+  const int row0 = sub * ROWS, row_end = min(rows, row0 + ROWS);
+  const int pos_lo = first_pos + row0 / p.group, pos_hi = first_pos + (row_end - 1) / p.group;
+  const int hi = max(0, pos_hi + 1);
+  const int lo = p.window ? max(0, pos_lo - p.window + 1) & ~(S::T - 1) : 0;
+  const int steps = hi > lo ? (hi - lo + S::T - 1) / S::T : 0;
+
+  // the lane's query row
+  const int row = row0 + 32 * wave + n;
+  const bool live = row < rows;
+  const int query = row / p.group;
+  const int pos = live ? first_pos + query : -1;
+  const int first = p.window ? pos - p.window + 1 : 0;
+  // tokens that all of the wave's live rows see
+  const int w_row = row0 + 32 * wave, w_last = min(rows - 1, w_row + 31);
+  const int all_hi = w_row < rows ? first_pos + w_row / p.group + 1 : 0x7fffffff;
+  const int all_lo = p.window && w_row < rows ? first_pos + w_last / p.group - p.window + 1 : 0;
+
+  bf16x8 qf[S::KS];
+  {
+    const bf16_t* src = static_cast<const bf16_t*>(p.q) +
+                        (live ? (q.q0 + query) * p.ldq + static_cast<int64_t>(h * p.group + row - query * p.group) * D : 0);
+#pragma unroll
+    for (int s = 0; s < S::KS; ++s) {
+      qf[s] = frag(0, 0, 0, 0);
+      if (live) qf[s] = *reinterpret_cast<const bf16x8*>(src + 16 * s + 8 * hh);
+    }
+  }
+  f32x16 o[S::DB];
+#pragma unroll
+  for (int d = 0; d < S::DB; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+  float m = -INFINITY, l = 0.0f;
+
+  // what the thread converts: 32 elements of one token's key, and 8 elements of four tokens' values
+  const bool does_k = kBoth || tid < 256, does_v = kBoth || tid >= 256;
+  const int k_tok = (tid & 255) % S::T, k_blk = (tid & 255) / S::T;
+  const int v_quad = (tid & 255) % (S::T / 4), v_eighth = (tid & 255) / (S::T / 4);
+  const int page_mask = (1 << p.c.page_shift) - 1;
+  const int32_t* const table = p.table + static_cast<int64_t>(b) * p.max_pages;
+  int k_page = 0, v_page = 0;
+  uint4 k_raw, v_raw;
+  uint32_t k_scale = 0, v_scale = 0;
+  // Tokens past the last seen one read its page's codes or its own; they are masked.
+  auto token = [&](int step, int off) { return min(lo + step * S::T + off, hi - 1); };
+  auto look_up = [&](int step) {
+    if (does_k) k_page = table[token(step, k_tok) >> p.c.page_shift];
+    if (does_v) v_page = table[token(step, 4 * v_quad) >> p.c.page_shift];
+  };
+  auto load = [&](int step) {
+    if (does_k) {
+      const bool bad = static_cast<uint32_t>(k_page) >= static_cast<uint32_t>(p.c.n_pages);
+      const int64_t at = ((static_cast<int64_t>(bad ? 0 : k_page) * p.c.heads + h) << p.c.page_shift) + (token(step, k_tok) & page_mask);
+      k_raw = *reinterpret_cast<const uint4*>(p.c.kc + at * (D / 2) + k_blk * 16);
+      k_scale = p.c.ks[at * S::DB + k_blk];
+      if (bad) k_scale = 0xffu;
+    }
+    if (does_v) {
+      const bool bad = static_cast<uint32_t>(v_page) >= static_cast<uint32_t>(p.c.n_pages);
+      const int64_t at = ((static_cast<int64_t>(bad ? 0 : v_page) * p.c.heads + h) << p.c.page_shift) +
+                         (token(step, 4 * v_quad) & page_mask & ~3);
+      v_raw = *reinterpret_cast<const uint4*>(p.c.vc + at * (D / 2) + v_eighth * 16);
+      v_scale = *reinterpret_cast<const uint32_t*>(p.c.vs + at * S::DB + (v_eighth >> 2) * 4);
+      if (bad) v_scale = 0xffffffffu;
+    }
+  };
+  // tokens of a step from here on, or before there, may be hidden from some row of the workgroup
+  const int wg_all_hi = pos_lo + 1, wg_all_lo = p.window ? pos_hi - p.window + 1 : 0;
+  auto convert = [&](int step) {
+    char* const kb = sh.k[step & 1];
+    char* const vb = sh.v[step & 1];
+    if (does_k) {
+      const uint32_t w[4] = {k_raw.x, k_raw.y, k_raw.z, k_raw.w};
+      const float unit = unit_of(k_scale, 0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<bf16x8*>(kb + S::key(k_tok, 4 * k_blk + i)) =
+            frag(fp4_pair(w[i], unit, 0), fp4_pair(w[i], unit, 1), fp4_pair(w[i], unit, 2), fp4_pair(w[i], unit, 3));
+    }
+    if (does_v) {
+      uint32_t w[4] = {v_raw.x, v_raw.y, v_raw.z, v_raw.w};
+      uint32_t scale = v_scale;
+      const int at = lo + step * S::T;
+      if (at + S::T > wg_all_hi || at < wg_all_lo) {
+        // A weight of zero does not hide a NaN: where rows may be masked, NaN
+        // blocks are taken out and noted, and the rows that see them made NaN.
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (((scale >> (8 * j)) & 0xffu) == 0xffu) {
+            const int tok = 4 * v_quad + j;
+            w[j] = 0;
+            scale ^= 0x80u << (8 * j);                                   // 255 -> 127
+            atomicOr(reinterpret_cast<unsigned long long*>(&sh.nan[step % 3][tok >> 6][v_eighth >> 2]), 1ull << (tok & 63));
+          }
+      }
+      uint32_t y[4][4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float unit = unit_of(scale, j);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[j][e] = fp4_pair(w[j], unit, e);
+      }
+      // four tokens of one element: half a piece
+      const int piece = (v_quad >> 2) * 2 + (v_quad & 1), half = 8 * ((v_quad >> 1) & 1);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int d = 8 * v_eighth + 2 * e;
+        *reinterpret_cast<uint2*>(vb + S::value(d, piece) + half) =
+            make_uint2(__builtin_amdgcn_perm(y[1][e], y[0][e], 0x05040100u), __builtin_amdgcn_perm(y[3][e], y[2][e], 0x05040100u));
+        *reinterpret_cast<uint2*>(vb + S::value(d + 1, piece) + half) =
+            make_uint2(__builtin_amdgcn_perm(y[1][e], y[0][e], 0x07060302u), __builtin_amdgcn_perm(y[3][e], y[2][e], 0x07060302u));
+      }
+    }
+  };
+  auto clear = [&](int which) {
+    for (int i = tid; i < static_cast<int>(sizeof(sh.nan[0]) / 8); i += 64 * WAVES) (&sh.nan[which][0][0])[i] = 0;
+  };
+
+  clear(0);
+  clear(1);
+  __syncthreads();
+  if (steps > 0) {
+    look_up(0);
+    load(0);
+    look_up(min(1, steps - 1));
+    convert(0);
+    load(min(1, steps - 1));
+    look_up(min(2, steps - 1));
+  }
+  for (int step = 0; step < steps; ++step) {
+    __syncthreads();
+    const char* const kb = sh.k[step & 1];
+    const char* const vb = sh.v[step & 1];
+    const int at = lo + step * S::T;
+    clear((step + 2) % 3);
+    f32x16 s[S::MB];
+#pragma unroll
+    for (int mb = 0; mb < S::MB; ++mb) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[mb][i] = 0.0f;
+#pragma unroll
+      for (int k = 0; k < S::KS; ++k)
+        s[mb] = mfma32(*reinterpret_cast<const bf16x8*>(kb + S::key(32 * mb + n, 2 * k + hh)), qf[k], s[mb]);
+    }
+    auto seen = [&](int mb, int i) {
+      const int tok = at + 32 * mb + 8 * (i >> 2) + 4 * hh + (i & 3);
+      return tok <= pos && tok >= first;
+    };
+    const bool masked = at + S::T > all_hi || at < all_lo;               // the same for the whole wave
+    if (masked) {
+#pragma unroll
+      for (int mb = 0; mb < S::MB; ++mb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (!seen(mb, i)) s[mb][i] = -INFINITY;
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int mb = 0; mb < S::MB; ++mb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[mb][i]);
+    {
+      const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+      top = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1])) * p.scale_log2e;
+    }
+    const float m_new = fmaxf(m, top);
+    const float base = m_new == -INFINITY ? 0.0f : m_new;
+    if (__any(m_new > m)) {
+      const float fade = __builtin_amdgcn_exp2f(m - base);
+      l *= fade;
+#pragma unroll
+      for (int d = 0; d < S::DB; ++d) o[d] *= fade;
+      m = m_new;
+    }
+    bf16x8 pf[S::MB][2];
+#pragma unroll
+    for (int mb = 0; mb < S::MB; ++mb) {
+      uint32_t w[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[mb][2 * i], p.scale_log2e, -base));
+        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[mb][2 * i + 1], p.scale_log2e, -base));
+        l += x + y;
+        w[i] = f32_to_bf16_pair(x, y);
+      }
+      pf[mb][0] = frag(w[0], w[1], w[2], w[3]);
+      pf[mb][1] = frag(w[4], w[5], w[6], w[7]);
+    }
+#pragma unroll
+    for (int mb = 0; mb < S::MB; ++mb)
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int d = 0; d < S::DB; ++d)
+          o[d] = mfma32(*reinterpret_cast<const bf16x8*>(vb + S::value(32 * d + n, (mb * 2 + k) * 2 + hh)), pf[mb][k], o[d]);
+    if (at + S::T > wg_all_hi || at < wg_all_lo) {
+#pragma unroll
+      for (int d = 0; d < S::DB; ++d)
+        for (int x = 0; x < (S::T + 63) / 64; ++x)
+          for (uint64_t hit = sh.nan[step % 3][x][d]; hit; hit &= hit - 1) {
+            const int tok = at + 64 * x + __builtin_ctzll(hit);
+            if (tok <= pos && tok >= first)
+#pragma unroll
+              for (int i = 0; i < 16; ++i) o[d][i] = NAN;
+          }
+    }
+    if (step + 1 < steps) {
+      convert(step + 1);
+      load(min(step + 2, steps - 1));
+      look_up(min(step + 3, steps - 1));
+    }
+  }
+  {
+    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+    l = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+  }
+  if (!live) return;
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  bf16_t* const out = static_cast<bf16_t*>(p.out) + (q.q0 + query) * p.ldo +
+                      static_cast<int64_t>(h * p.group + row - query * p.group) * D;
+#pragma unroll
+  for (int d = 0; d < S::DB; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      const float f[4] = {o[d][i] * inv, o[d][i + 1] * inv, o[d][i + 2] * inv, o[d][i + 3] * inv};
+      store_out<4>(out + 32 * d + 2 * i + 4 * hh, f);
+    }
+}
+
+template <int D, int WAVES> hipError_t launch(const AttnParams& p, hipStream_t s) {
+  const int64_t all = static_cast<int64_t>(p.T) * p.group, rows = 32 * WAVES;
+  const int64_t tiles = (all + rows - 1) / rows + std::min<int64_t>(p.B, all / kSmallRows);
+  attn_prompt_kernel<D, WAVES><<<static_cast<uint32_t>(tiles * p.c.heads), 64 * WAVES, 0, s>>>(p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_attention_prompts(const AttnParams& p, hipStream_t s) {
+  switch (p.c.d) {
+    case 64: return launch<64, 8>(p, s);
+    case 128: return launch<128, 8>(p, s);
+    default: return launch<256, 4>(p, s);
+  }
+}
+
+}  // namespace cts

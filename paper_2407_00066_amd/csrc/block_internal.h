@@ -44,6 +44,8 @@ bool plan_attention(AttnParams* p, size_t* bytes);
 // Lays the workspace out for the plan.
 void place_attention(AttnParams* p, void* workspace);
 hipError_t launch_attention(const AttnParams& p, hipStream_t s);
+// The bf16 sequences with many query rows (attention_tile.hip).
+hipError_t launch_attention_prompts(const AttnParams& p, hipStream_t s);
 
 struct NormParams {
   int T, d;
