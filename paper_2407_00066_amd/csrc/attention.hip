@@ -44,9 +44,9 @@ __device__ __forceinline__ void attend(const AttnParams& p, const Tile& t, int h
   const int query = row / p.group;
   const int pos = live ? t.first_pos + query : -1;                      // sees tokens first .. pos
   const int first = p.window ? pos - p.window + 1 : 0;
-  auto seen = [&](int at, int i, int j) {
-    const int tok = at + 16 * i + 4 * g + j;
-    return tok <= pos && tok >= first;
+  auto seen = [&](int from, int i, int j) {                              // token from + a constant
+    const int tok = 16 * i + j;
+    return tok <= pos - from && tok >= first - from;
   };
 
   bf16x8 qf[KS][NS];
@@ -165,19 +165,19 @@ __device__ __forceinline__ void attend(const AttnParams& p, const Tile& t, int h
     for (int i = 0; i < 8; ++i) sc[i] = x[i >> 2][i & 3] * p.scale_log2e;
     const bool masked = at + kUnit > all_hi || at < all_lo;              // the same for the whole wave
     if (masked) {
+      const int from = rare(at + 4 * g);
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          if (!seen(at, i, j)) sc[4 * i + j] = -INFINITY;
+          if (!seen(from, i, j)) sc[4 * i + j] = -INFINITY;
     }
     float top = sc[0];
 #pragma unroll
     for (int i = 1; i < 8; ++i) top = fmaxf(top, sc[i]);
-    const float m_new = fmaxf(st.m, max_over_groups(top));
-    const float base = m_new == -INFINITY ? 0.0f : m_new;
-    if (__any(m_new > st.m)) {                                           // seldom after the first steps
-      const float fade = __builtin_amdgcn_exp2f(st.m - base);
+    top = max_over_groups(top);
+    if (__any(top > st.m + kSlack)) {
+      const float m_new = fmaxf(st.m, top), fade = __builtin_amdgcn_exp2f(st.m - (m_new == -INFINITY ? 0.0f : m_new));
       st.l *= fade;
 #pragma unroll
       for (int c = 0; c < NC; ++c)
@@ -185,6 +185,7 @@ __device__ __forceinline__ void attend(const AttnParams& p, const Tile& t, int h
         for (int e = 0; e < NB; ++e) st.o[c][e] *= fade;
       st.m = m_new;
     }
+    const float base = st.m == -INFINITY ? 0.0f : st.m;
     float w[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -204,14 +205,14 @@ __device__ __forceinline__ void attend(const AttnParams& p, const Tile& t, int h
         for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            if (((vs[i][c] >> (8 * j)) & 0xffu) == 0xffu) hit[2 * i + j / 2] |= 0x3f80u << (16 * (j & 1));
+            if (((rare(static_cast<int>(vs[i][c])) >> (8 * j)) & 0xff) == 0xff) hit[2 * i + j / 2] |= 0x3f80u << (16 * (j & 1));
         if (__any((hit[0] | hit[1] | hit[2] | hit[3]) != 0)) {
           float in[8];
 #pragma unroll
           for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              in[4 * i + j] = seen(at, i, j) ? 1.0f : 0.0f;
+              in[4 * i + j] = seen(at + 4 * g, i, j) ? 1.0f : 0.0f;
               if (((vs[i][c] >> (8 * j)) & 0xffu) == 0xffu) {
                 vs[i][c] ^= 0x80u << (8 * j);                            // 255 -> 127
                 (&v[i][c].x)[j] = 0;

@@ -12,6 +12,11 @@ constexpr int kSmallRows = 64;     // rows of a sequence that the 16-row tiles a
 constexpr int kRuns = 4096;        // waves that a batch's steps are dealt out to: 16 for every compute unit
 constexpr int kMinRun = 4;         // steps of a run, at least
 constexpr int kJoinThreads = 256;
+// The sums follow the running maximum only once it has grown by 2^8: until then
+// weights are up to 2^8 instead of 1, which costs no precision in floats (nor in
+// bf16), and the sums are seldom rescaled.  The weight that a row's maximum came
+// from stays 1, so its length is 0 only where it has seen nothing.
+constexpr float kSlack = 8.0f;
 
 __device__ __forceinline__ uint32_t fp4_pair(uint32_t w, float unit, int byte) {
   switch (byte) {
@@ -22,6 +27,15 @@ __device__ __forceinline__ uint32_t fp4_pair(uint32_t w, float unit, int byte) {
   }
 }
 
+// v as computed here and not before: in a branch that is seldom taken, what is
+// computed from it stays there (the compiler otherwise works both sides out every
+// time and selects; masks alone are a third of a step's vector instructions).
+__device__ __forceinline__ int rare(int v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("" : "+v"(v));
+#endif
+  return v;
+}
 // the float 2^(s - 127) of byte i of w (255: as the conversion's NaN scale)
 __device__ __forceinline__ float unit_of(uint32_t w, int i) {
   return __uint_as_float((i < 3 ? w << (23 - 8 * i) : w >> 1) & 0x7f800000u);

@@ -28,6 +28,10 @@ __device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
 
+#ifndef W128
+#define W128 4
+#endif
+#define WAVES_LB (D == 256 ? 1 : 2)
 template <int D> struct Step {
   static constexpr int T = 8192 / D;               // tokens
   static constexpr int MB = T / 32;                // row blocks of the first product
@@ -46,7 +50,7 @@ template <int D> struct TileShared {
 };
 
 template <int D, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attn_prompt_kernel(AttnParams p) {
+__global__ __launch_bounds__(64 * WAVES, WAVES_LB) void attn_prompt_kernel(AttnParams p) {
   using S = Step<D>;
   constexpr int ROWS = 32 * WAVES;
   constexpr bool kBoth = WAVES == 4;               // 512 threads: half of them convert keys, half values; 256: all both
@@ -198,6 +202,9 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attn_prompt_kern
     for (int i = tid; i < static_cast<int>(sizeof(sh.nan[0]) / 8); i += 64 * WAVES) (&sh.nan[which][0][0])[i] = 0;
   };
 
+#ifdef PRW
+  if ((blockIdx.x >> 8) & 1) __builtin_amdgcn_s_setprio(1);
+#endif
   clear(0);
   clear(1);
   __syncthreads();
@@ -224,17 +231,17 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attn_prompt_kern
       for (int k = 0; k < S::KS; ++k)
         s[mb] = mfma32(*reinterpret_cast<const bf16x8*>(kb + S::key(32 * mb + n, 2 * k + hh)), qf[k], s[mb]);
     }
-    auto seen = [&](int mb, int i) {
-      const int tok = at + 32 * mb + 8 * (i >> 2) + 4 * hh + (i & 3);
-      return tok <= pos && tok >= first;
-    };
     const bool masked = at + S::T > all_hi || at < all_lo;               // the same for the whole wave
     if (masked) {
+      // register i is token at + 4 hh + a constant
+      const int from = rare(at + 4 * hh), below = pos - from, above = first - from;
 #pragma unroll
       for (int mb = 0; mb < S::MB; ++mb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (!seen(mb, i)) s[mb][i] = -INFINITY;
+        for (int i = 0; i < 16; ++i) {
+          const int tok = 32 * mb + 8 * (i >> 2) + (i & 3);
+          if (tok > below || tok < above) s[mb][i] = -INFINITY;
+        }
     }
     float top = s[0][0];
 #pragma unroll
@@ -245,15 +252,14 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attn_prompt_kern
       const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
       top = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1])) * p.scale_log2e;
     }
-    const float m_new = fmaxf(m, top);
-    const float base = m_new == -INFINITY ? 0.0f : m_new;
-    if (__any(m_new > m)) {
-      const float fade = __builtin_amdgcn_exp2f(m - base);
+    if (__any(top > m + kSlack)) {
+      const float m_new = fmaxf(m, top), fade = __builtin_amdgcn_exp2f(m - (m_new == -INFINITY ? 0.0f : m_new));
       l *= fade;
 #pragma unroll
       for (int d = 0; d < S::DB; ++d) o[d] *= fade;
       m = m_new;
     }
+    const float base = m == -INFINITY ? 0.0f : m;
     bf16x8 pf[S::MB][2];
 #pragma unroll
     for (int mb = 0; mb < S::MB; ++mb) {
@@ -262,8 +268,8 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void attn_prompt_kern
       for (int i = 0; i < 8; ++i) {
         const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[mb][2 * i], p.scale_log2e, -base));
         const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[mb][2 * i + 1], p.scale_log2e, -base));
-        l += x + y;
         w[i] = f32_to_bf16_pair(x, y);
+        l += x + y;
       }
       pf[mb][0] = frag(w[0], w[1], w[2], w[3]);
       pf[mb][1] = frag(w[4], w[5], w[6], w[7]);
@@ -320,8 +326,8 @@ template <int D, int WAVES> hipError_t launch(const AttnParams& p, hipStream_t s
 
 hipError_t launch_attention_prompts(const AttnParams& p, hipStream_t s) {
   switch (p.c.d) {
-    case 64: return launch<64, 8>(p, s);
-    case 128: return launch<128, 8>(p, s);
+    case 64: return launch<64, 4>(p, s);
+    case 128: return launch<128, W128>(p, s);
     default: return launch<256, 4>(p, s);
   }
 }
