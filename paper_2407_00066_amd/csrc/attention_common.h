@@ -12,6 +12,9 @@ constexpr int kSmallRows = 64;     // rows of a sequence that the 16-row tiles a
 constexpr int kRuns = 4096;        // waves that a batch's steps are dealt out to: 16 for every compute unit
 constexpr int kMinRun = 4;         // steps of a run, at least
 constexpr int kJoinThreads = 256;
+constexpr int kPromptRows = 128;   // query rows of a workgroup for prompts
+constexpr int64_t kPromptGroups = 512;  // workgroups that few prompts are split into: two for every compute unit
+constexpr int64_t kPromptSteps = 8;     // steps of 8192 / d tokens of a piece, at least
 // The sums follow the running maximum only once it has grown by 2^8: until then
 // weights are up to 2^8 instead of 1, which costs no precision in floats (nor in
 // bf16), and the sums are seldom rescaled.  The weight that a row's maximum came

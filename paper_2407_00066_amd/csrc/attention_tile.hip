@@ -18,9 +18,12 @@
 #include <algorithm>
 
 #include "attention_common.h"
+#include "ldsdma.h"
 
 namespace cts {
 namespace {
+
+constexpr int kThreads = 256, kRows = kPromptRows;
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
@@ -28,42 +31,30 @@ __device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
 
-#ifndef W128
-#define W128 4
-#endif
-#define WAVES_LB (D == 256 ? 1 : 2)
 template <int D> struct Step {
   static constexpr int T = 8192 / D;               // tokens
   static constexpr int MB = T / 32;                // row blocks of the first product
   static constexpr int DB = D / 32;                // row blocks of the second; scale blocks
   static constexpr int KS = D / 16;                // k steps of the first
   static constexpr int KC = D / 8, VC = T / 8;     // 16-byte pieces of a row of keys, of values
-  static __device__ __forceinline__ int key(int tok, int c) { return (tok * KC + (c ^ (tok & (KC < 16 ? KC - 1 : 15)))) * 16; }
+  // Sixteen lanes reading a piece of sixteen rows meet no bank twice (256 bytes wide).
+  static __device__ __forceinline__ int key(int tok, int c) {
+    return (tok * KC + (c ^ (KC == 8 ? (tok >> 1) & 7 : tok & 15))) * 16;
+  }
   static __device__ __forceinline__ int value(int d, int c) {
-    return (d * VC + (c ^ (VC == 4 ? (d >> 1) & 3 : d & (VC - 1)))) * 16;
+    return (d * VC + (c ^ (VC == 4 ? (d >> 2) & 3 : VC == 8 ? (d >> 1) & 7 : d & 15))) * 16;
   }
 };
 
-template <int D> struct TileShared {
-  char k[2][8192 * 2], v[2][8192 * 2];
-  uint64_t nan[3][(Step<D>::T + 63) / 64][Step<D>::DB];                  // tokens whose value block is NaN
-};
-
-template <int D, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, WAVES_LB) void attn_prompt_kernel(AttnParams p) {
-  using S = Step<D>;
-  constexpr int ROWS = 32 * WAVES;
-  constexpr bool kBoth = WAVES == 4;               // 512 threads: half of them convert keys, half values; 256: all both
-  __shared__ TileShared<D> sh;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int n = lane & 31, hh = lane >> 5;
-  const int index = blockIdx.x / p.c.heads, h = blockIdx.x - index * p.c.heads;
-  int b = -1, sub = 0;
-  for (int base = 0, before = 0; base < p.B && b < 0; base += 64) {
+// Tile `index` of the sequences with many rows: their number is known on the
+// device only, so the lanes count.  False: there are not so many.
+__device__ __forceinline__ bool find_tile(const AttnParams& p, int index, int* b, int* sub) {
+  const int lane = threadIdx.x & 63;
+  for (int base = 0, before = 0; base < p.B; base += 64) {
     int count = 0;
     if (base + lane < p.B) {
       const int rows = min(queries_of(p, base + lane).n, p.max_q) * p.group;
-      count = rows > kSmallRows ? (rows + ROWS - 1) / ROWS : 0;
+      count = rows > kSmallRows ? (rows + kRows - 1) / kRows : 0;
     }
     int to = count;
 #pragma unroll
@@ -74,21 +65,41 @@ __global__ __launch_bounds__(64 * WAVES, WAVES_LB) void attn_prompt_kernel(AttnP
     const uint64_t here = __ballot(before + to > index);
     if (here) {
       const int at = __builtin_ctzll(here);
-      b = base + at;
+      *b = base + at;
       // a sequence's last rows see most: they go first
-      sub = before + __builtin_amdgcn_readlane(to, at) - 1 - index;
+      *sub = before + __builtin_amdgcn_readlane(to, at) - 1 - index;
+      return true;
     }
     before += __builtin_amdgcn_readlane(to, 63);
   }
-  if (b < 0) return;
+  return false;
+}
+
+template <int D> struct TileShared {
+  char k[2][8192 * 2], v[2][8192 * 2];
+  uint64_t nan[3][(Step<D>::T + 63) / 64][Step<D>::DB];                  // tokens whose value block is NaN
+};
+
+template <int D>
+__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prompt_kernel(AttnParams p) {
+  using S = Step<D>;
+  __shared__ TileShared<D> sh;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 31, hh = lane >> 5;
+  const int item = blockIdx.x / p.pieces, piece = blockIdx.x - item * p.pieces;
+  const int h = item % p.c.heads;
+  int b, sub;
+  if (!find_tile(p, item / p.c.heads, &b, &sub)) return;
   const Queries q = queries_of(p, b);
   const int len = min(max(p.kv_len[b], 0), p.max_kv);
   const int rows = min(q.n, p.max_q) * p.group, first_pos = len - q.n;
-  const int row0 = sub * ROWS, row_end = min(rows, row0 + ROWS);
+  const int row0 = sub * kRows, row_end = min(rows, row0 + kRows);
   const int pos_lo = first_pos + row0 / p.group, pos_hi = first_pos + (row_end - 1) / p.group;
   const int hi = max(0, pos_hi + 1);
   const int lo = p.window ? max(0, pos_lo - p.window + 1) & ~(S::T - 1) : 0;
-  const int steps = hi > lo ? (hi - lo + S::T - 1) / S::T : 0;
+  const int all_steps = hi > lo ? (hi - lo + S::T - 1) / S::T : 0;
+  const int begin = static_cast<int>(static_cast<int64_t>(all_steps) * piece / p.pieces);
+  const int steps = static_cast<int>(static_cast<int64_t>(all_steps) * (piece + 1) / p.pieces);      // [begin, steps)
 
   // the lane's query row
   const int row = row0 + 32 * wave + n;
@@ -119,9 +130,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES_LB) void attn_prompt_kernel(AttnP
   float m = -INFINITY, l = 0.0f;
 
   // what the thread converts: 32 elements of one token's key, and 8 elements of four tokens' values
-  const bool does_k = kBoth || tid < 256, does_v = kBoth || tid >= 256;
-  const int k_tok = (tid & 255) % S::T, k_blk = (tid & 255) / S::T;
-  const int v_quad = (tid & 255) % (S::T / 4), v_eighth = (tid & 255) / (S::T / 4);
+  const int k_tok = tid % S::T, k_blk = tid / S::T;
+  const int v_quad = tid % (S::T / 4), v_eighth = tid / (S::T / 4);
   const int page_mask = (1 << p.c.page_shift) - 1;
   const int32_t* const table = p.table + static_cast<int64_t>(b) * p.max_pages;
   int k_page = 0, v_page = 0;
@@ -130,18 +140,18 @@ __global__ __launch_bounds__(64 * WAVES, WAVES_LB) void attn_prompt_kernel(AttnP
   // Tokens past the last seen one read its page's codes or its own; they are masked.
   auto token = [&](int step, int off) { return min(lo + step * S::T + off, hi - 1); };
   auto look_up = [&](int step) {
-    if (does_k) k_page = table[token(step, k_tok) >> p.c.page_shift];
-    if (does_v) v_page = table[token(step, 4 * v_quad) >> p.c.page_shift];
+    k_page = table[token(step, k_tok) >> p.c.page_shift];
+    v_page = table[token(step, 4 * v_quad) >> p.c.page_shift];
   };
   auto load = [&](int step) {
-    if (does_k) {
+    {
       const bool bad = static_cast<uint32_t>(k_page) >= static_cast<uint32_t>(p.c.n_pages);
       const int64_t at = ((static_cast<int64_t>(bad ? 0 : k_page) * p.c.heads + h) << p.c.page_shift) + (token(step, k_tok) & page_mask);
       k_raw = *reinterpret_cast<const uint4*>(p.c.kc + at * (D / 2) + k_blk * 16);
       k_scale = p.c.ks[at * S::DB + k_blk];
       if (bad) k_scale = 0xffu;
     }
-    if (does_v) {
+    {
       const bool bad = static_cast<uint32_t>(v_page) >= static_cast<uint32_t>(p.c.n_pages);
       const int64_t at = ((static_cast<int64_t>(bad ? 0 : v_page) * p.c.heads + h) << p.c.page_shift) +
                          (token(step, 4 * v_quad) & page_mask & ~3);
@@ -155,7 +165,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES_LB) void attn_prompt_kernel(AttnP
   auto convert = [&](int step) {
     char* const kb = sh.k[step & 1];
     char* const vb = sh.v[step & 1];
-    if (does_k) {
+    {
       const uint32_t w[4] = {k_raw.x, k_raw.y, k_raw.z, k_raw.w};
       const float unit = unit_of(k_scale, 0);
 #pragma unroll
@@ -163,7 +173,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES_LB) void attn_prompt_kernel(AttnP
         *reinterpret_cast<bf16x8*>(kb + S::key(k_tok, 4 * k_blk + i)) =
             frag(fp4_pair(w[i], unit, 0), fp4_pair(w[i], unit, 1), fp4_pair(w[i], unit, 2), fp4_pair(w[i], unit, 3));
     }
-    if (does_v) {
+    {
       uint32_t w[4] = {v_raw.x, v_raw.y, v_raw.z, v_raw.w};
       uint32_t scale = v_scale;
       const int at = lo + step * S::T;
@@ -199,7 +209,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES_LB) void attn_prompt_kernel(AttnP
     }
   };
   auto clear = [&](int which) {
-    for (int i = tid; i < static_cast<int>(sizeof(sh.nan[0]) / 8); i += 64 * WAVES) (&sh.nan[which][0][0])[i] = 0;
+    for (int i = tid; i < static_cast<int>(sizeof(sh.nan[0]) / 8); i += kThreads) (&sh.nan[which][0][0])[i] = 0;
   };
 
 #ifdef PRW
@@ -207,17 +217,19 @@ __global__ __launch_bounds__(64 * WAVES, WAVES_LB) void attn_prompt_kernel(AttnP
 #endif
   clear(0);
   clear(1);
+  clear(2);
   __syncthreads();
-  if (steps > 0) {
-    look_up(0);
-    load(0);
-    look_up(min(1, steps - 1));
-    convert(0);
-    load(min(1, steps - 1));
-    look_up(min(2, steps - 1));
+  const int last = steps - 1;
+  if (begin < steps) {
+    look_up(begin);
+    load(begin);
+    look_up(min(begin + 1, last));
+    convert(begin);
+    load(min(begin + 1, last));
+    look_up(min(begin + 2, last));
   }
-  for (int step = 0; step < steps; ++step) {
-    __syncthreads();
+  for (int step = begin; step < steps; ++step) {
+    lds_barrier();
     const char* const kb = sh.k[step & 1];
     const char* const vb = sh.v[step & 1];
     const int at = lo + step * S::T;
@@ -292,10 +304,10 @@ __global__ __launch_bounds__(64 * WAVES, WAVES_LB) void attn_prompt_kernel(AttnP
               for (int i = 0; i < 16; ++i) o[d][i] = NAN;
           }
     }
-    if (step + 1 < steps) {
+    if (step < last) {
       convert(step + 1);
-      load(min(step + 2, steps - 1));
-      look_up(min(step + 3, steps - 1));
+      load(min(step + 2, last));
+      look_up(min(step + 3, last));
     }
   }
   {
@@ -303,22 +315,72 @@ __global__ __launch_bounds__(64 * WAVES, WAVES_LB) void attn_prompt_kernel(AttnP
     l = __uint_as_float(x[0]) + __uint_as_float(x[1]);
   }
   if (!live) return;
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  bf16_t* const out = static_cast<bf16_t*>(p.out) + (q.q0 + query) * p.ldo +
-                      static_cast<int64_t>(h * p.group + row - query * p.group) * D;
+  if (p.pieces == 1) {
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    bf16_t* const out = static_cast<bf16_t*>(p.out) + (q.q0 + query) * p.ldo +
+                        static_cast<int64_t>(h * p.group + row - query * p.group) * D;
 #pragma unroll
-  for (int d = 0; d < S::DB; ++d)
+    for (int d = 0; d < S::DB; ++d)
 #pragma unroll
-    for (int i = 0; i < 16; i += 4) {
-      const float f[4] = {o[d][i] * inv, o[d][i + 1] * inv, o[d][i + 2] * inv, o[d][i + 3] * inv};
-      store_out<4>(out + 32 * d + 2 * i + 4 * hh, f);
-    }
+      for (int i = 0; i < 16; i += 4) {
+        const float f[4] = {o[d][i] * inv, o[d][i + 1] * inv, o[d][i + 2] * inv, o[d][i + 3] * inv};
+        store_out<4>(out + 32 * d + 2 * i + 4 * hh, f);
+      }
+  } else {
+    const int64_t at = static_cast<int64_t>(blockIdx.x) * kRows + 32 * wave + n;
+    float* const out = p.prompt_part + at * D;
+#pragma unroll
+    for (int d = 0; d < S::DB; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        const float f[4] = {o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]};
+        store_out<4>(out + 32 * d + 2 * i + 4 * hh, f);
+      }
+    if (hh == 0) *reinterpret_cast<float2*>(p.prompt_ml + 2 * at) = make_float2(m, l);
+  }
 }
 
-template <int D, int WAVES> hipError_t launch(const AttnParams& p, hipStream_t s) {
-  const int64_t all = static_cast<int64_t>(p.T) * p.group, rows = 32 * WAVES;
-  const int64_t tiles = (all + rows - 1) / rows + std::min<int64_t>(p.B, all / kSmallRows);
-  attn_prompt_kernel<D, WAVES><<<static_cast<uint32_t>(tiles * p.c.heads), 64 * WAVES, 0, s>>>(p);
+// Joins the pieces of tile blockIdx.x (tile x head), in their order: a thread takes
+// eight elements of one row.
+template <int D>
+__global__ __launch_bounds__(kThreads) void attn_prompt_join_kernel(AttnParams p) {
+  constexpr int kPer = kThreads / (D / 8);           // rows of a workgroup
+  const int h = blockIdx.x % p.c.heads;
+  int b, sub;
+  if (!find_tile(p, blockIdx.x / p.c.heads, &b, &sub)) return;
+  const Queries q = queries_of(p, b);
+  const int r = blockIdx.y * kPer + threadIdx.x / (D / 8), e = threadIdx.x % (D / 8) * 8;
+  const int row = sub * kRows + r, query = row / p.group;
+  if (row >= min(q.n, p.max_q) * p.group) return;
+  float M = -INFINITY;
+  for (int k = 0; k < p.pieces; ++k) {
+    const int64_t at = (static_cast<int64_t>(blockIdx.x) * p.pieces + k) * kRows + r;
+    M = fmaxf(M, p.prompt_ml[2 * at]);
+  }
+  const float base = M == -INFINITY ? 0.0f : M;
+  float L = 0.0f, f[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll 4
+  for (int k = 0; k < p.pieces; ++k) {
+    const int64_t at = (static_cast<int64_t>(blockIdx.x) * p.pieces + k) * kRows + r;
+    const float2 ml = *reinterpret_cast<const float2*>(p.prompt_ml + 2 * at);
+    const float4* o = reinterpret_cast<const float4*>(p.prompt_part + at * D + e);
+    const float4 x = o[0], y = o[1];
+    const float a = __builtin_amdgcn_exp2f(ml.x - base);
+    L += a * ml.y;
+    f[0] += a * x.x; f[1] += a * x.y; f[2] += a * x.z; f[3] += a * x.w;
+    f[4] += a * y.x; f[5] += a * y.y; f[6] += a * y.z; f[7] += a * y.w;
+  }
+  const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] *= inv;
+  store_out<8>(static_cast<bf16_t*>(p.out) + (q.q0 + query) * p.ldo +
+                   static_cast<int64_t>(h * p.group + row - query * p.group) * D + e, f);
+}
+
+template <int D> hipError_t launch(const AttnParams& p, hipStream_t s) {
+  const uint32_t tiles = static_cast<uint32_t>(p.prompt_tiles * p.c.heads);
+  attn_prompt_kernel<D><<<tiles * p.pieces, kThreads, 0, s>>>(p);
+  if (p.pieces > 1) attn_prompt_join_kernel<D><<<dim3(tiles, kRows * (D / 8) / kThreads), kThreads, 0, s>>>(p);
   return hipGetLastError();
 }
 
@@ -326,9 +388,9 @@ template <int D, int WAVES> hipError_t launch(const AttnParams& p, hipStream_t s
 
 hipError_t launch_attention_prompts(const AttnParams& p, hipStream_t s) {
   switch (p.c.d) {
-    case 64: return launch<64, 4>(p, s);
-    case 128: return launch<128, W128>(p, s);
-    default: return launch<256, 4>(p, s);
+    case 64: return launch<64>(p, s);
+    case 128: return launch<128>(p, s);
+    default: return launch<256>(p, s);
   }
 }
 

@@ -36,6 +36,11 @@ struct AttnParams {
   int64_t large_tiles;
   float *part, *part_ml;            // [2 runs][part_rows][d] sums, [2 runs][part_rows][2] maxima and lengths
   int32_t* info;                    // [tiles][kv heads][4] a tile's pieces, the first one's slot, its query row, first row and rows
+  // prompts in bf16: workgroup tiles, pieces of a tile's tokens, and with more than one their
+  // sums [tiles][kv heads][pieces][128][d], maxima and lengths [..][128][2]
+  int64_t prompt_tiles;
+  int pieces;
+  float *prompt_part, *prompt_ml;
 };
 
 // Chooses the plan and gives the workspace's bytes (not falling with any size);
