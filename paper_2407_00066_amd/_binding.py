@@ -20,22 +20,33 @@ _lib = None
 _lock = threading.Lock()
 
 
-def _load_address():
-    """_marshal's tensor check, or (no fallback) a stand-in whose every call says
-    why it cannot be used."""
+class _Unusable:
+    """Stands in for _marshal where it cannot be used (no fallback): every call says why."""
+
+    def __init__(self, why):
+        self._why = why
+
+    def __getattr__(self, name):
+        def refuse(*_):
+            raise RuntimeError("_marshal.so is not built or does not load (%s); run "
+                               "`python -m paper_2407_00066_amd.build`" % self._why)
+        return refuse
+
+
+def _load_marshal():
     try:
         from . import _marshal
         built_for = getattr(_marshal, "built_for", "another torch")
         if built_for == torch.__version__:
-            return _marshal.address
-        why = "it was built for torch %s, this is %s" % (built_for, torch.__version__)
+            return _marshal
+        return _Unusable("it was built for torch %s, this is %s" % (built_for, torch.__version__))
     except ImportError as e:
-        why = str(e)
+        return _Unusable(str(e))
 
-    def address(*_):
-        raise RuntimeError("_marshal.so is not built or does not load (%s); run "
-                           "`python -m paper_2407_00066_amd.build`" % why)
-    return address
+
+def _load_address():
+    """_marshal's tensor check."""
+    return _load_marshal().address
 
 
 _address = _load_address()

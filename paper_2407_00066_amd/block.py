@@ -13,9 +13,34 @@ import ctypes
 
 import torch
 
-from ._binding import AttnProblem, KvCacheArrays, _check, _check_tensor, _dev, _dt, _stream, _workspace, lib
+from . import _binding
+from ._binding import AttnProblem, KvCacheArrays, _check, _check_tensor, _dev, _dt, _load_marshal, _stream, lib
 
 U8, I32, I64, F32 = torch.uint8, torch.int32, torch.int64, torch.float32
+
+# The calls are made natively (a decode step's take the GPU a few microseconds
+# each); where one refuses an argument, the functions below find out which.
+_native = _load_marshal()
+_entries: dict = {}
+
+
+def _entry(name: str) -> int:
+    """The address of a C entry point."""
+    at = _entries.get(name)
+    if at is None:
+        at = _entries[name] = ctypes.cast(getattr(lib(), name), ctypes.c_void_p).value
+    return at
+
+
+def _raw_stream(device: torch.device) -> int:
+    return _stream(device) if device.type == "cuda" else 0
+
+
+def _refused(device: torch.device, where: str):
+    """The checks of a call that was refused have found nothing wrong with its tensors."""
+    if device.type != "cuda":
+        raise ValueError("%s: tensors must be on a GPU, not on %s" % (where, device))
+    raise ValueError("%s: arguments must be plain tensors and 32-bit sizes" % where)
 
 
 class KVCache:
@@ -40,6 +65,7 @@ class KVCache:
               _dev(v_codes, "v_codes", dev, U8, (n, h, s // 4, d // 8, 4, 4)),
               _dev(v_scales, "v_scales", dev, U8, (n, h, s // 4, d // 32, 4))]
         self._c = KvCacheArrays(n, s, h, d, *at)
+        self._at = ctypes.addressof(self._c)
 
     @property
     def n_slots(self) -> int:
@@ -73,40 +99,41 @@ def _rows(t, name, device, dtype, shape):
 def kv_write(cache: KVCache, k, v, slots) -> None:
     """Quantises k, v [T, heads, head_dim] into the cache's slots [T] (int64,
     page * page_size + offset; outside the cache: skipped).  See cts_kv_write."""
-    dev, T = cache.device, k.shape[0]
-    shape = (T, cache.n_heads, cache.head_dim)
-    dt = _dt(k, "k")
-    kp, ldk = _rows(k, "k", dev, k.dtype, shape)
-    vp, ldv = _rows(v, "v", dev, k.dtype, shape)
-    _check(lib().cts_kv_write(ctypes.byref(cache._c), T, kp, ldk, vp, ldv, _dev(slots, "slots", dev, I64, (T,)), dt,
-                              _stream(dev)), "cts_kv_write")
+    dev = cache.device
+    st = _native.kv_write(_entry("cts_kv_write"), _raw_stream(dev), dev, cache._at, k, v, slots)
+    if st is None:
+        _dt(k, "k")
+        shape = (k.shape[0], cache.n_heads, cache.head_dim)
+        _rows(k, "k", dev, k.dtype, shape)
+        _rows(v, "v", dev, k.dtype, shape)
+        _dev(slots, "slots", dev, I64, (shape[0],))
+        _refused(dev, "kv_write")
+    _check(st, "cts_kv_write")
 
 
 def kv_read(cache: KVCache, slots, dtype=torch.bfloat16, k_out=None, v_out=None):
     """(k, v) [T, heads, head_dim]: what the cache holds for slots [T] (outside
     the cache: zeros).  See cts_kv_read."""
-    dev, T = cache.device, slots.numel()
-    shape = (T, cache.n_heads, cache.head_dim)
-    k = torch.empty(shape, dtype=dtype, device=dev) if k_out is None else k_out
-    v = torch.empty(shape, dtype=k.dtype, device=dev) if v_out is None else v_out
-    dt = _dt(k, "k_out")
-    kp, ldk = _rows(k, "k_out", dev, k.dtype, shape)
-    vp, ldv = _rows(v, "v_out", dev, k.dtype, shape)
-    _check(lib().cts_kv_read(ctypes.byref(cache._c), T, _dev(slots, "slots", dev, I64, (T,)), kp, ldk, vp, ldv, dt,
-                             _stream(dev)), "cts_kv_read")
-    return k, v
-
-
-def _attn_problem(q, cache, B, max_pages, max_q, max_kv, window, scale):
-    T, heads = q.shape[0], q.shape[1]
-    return AttnProblem(T, B, heads, max_pages, max_q, max_kv, window, _dt(q, "q"),
-                       cache.head_dim ** -0.5 if scale is None else scale)
+    dev = cache.device
+    r = _native.kv_read(_entry("cts_kv_read"), _raw_stream(dev), dev, cache._at, slots, dtype, k_out, v_out)
+    if r is None:
+        shape = (slots.numel(), cache.n_heads, cache.head_dim)
+        _dev(slots, "slots", dev, I64, (shape[0],))
+        if k_out is not None:
+            dtype = k_out.dtype
+        _dt(torch.empty(0, dtype=dtype), "the output")
+        for t, name in ((k_out, "k_out"), (v_out, "v_out")):
+            if t is not None:
+                _rows(t, name, dev, dtype, shape)
+        _refused(dev, "kv_read")
+    _check(r[2], "cts_kv_read")
+    return r[0], r[1]
 
 
 def kv_attention_workspace_size(q, cache: KVCache, B, max_q, max_kv, window=0) -> int:
     """Bytes of workspace kv_attention needs for queries like q of B sequences
     (0 for a call it would refuse)."""
-    p = _attn_problem(q, cache, B, max(1, -(-max_kv // cache.page_size)), max_q, max_kv, window, 1.0)
+    p = AttnProblem(q.shape[0], B, q.shape[1], max(1, -(-max_kv // cache.page_size)), max_q, max_kv, window, _dt(q, "q"), 1.0)
     return int(lib().cts_kv_attention_workspace_size(ctypes.byref(p), ctypes.byref(cache._c)))
 
 
@@ -118,23 +145,25 @@ def kv_attention(q, cache: KVCache, block_table, kv_len, q_start=None, max_q=1, 
     and max_kv bound the queries of a sequence and kv_len (max_kv None: what the
     table has room for).  scale None: head_dim^-1/2.  See cts_kv_attention."""
     dev = cache.device
-    T, heads = q.shape[0], q.shape[1]
-    B, max_pages = block_table.shape
-    shape = (T, heads, cache.head_dim)
-    qp, ldq = _rows(q, "q", dev, q.dtype, shape)
-    if out is None:
-        out = torch.empty(shape, dtype=q.dtype, device=dev)
-    op, ldo = _rows(out, "out", dev, q.dtype, shape)
-    p = _attn_problem(q, cache, B, max_pages, max_q, max_pages * cache.page_size if max_kv is None else max_kv, window,
-                      scale)
-    c = ctypes.byref(cache._c)
-    args = (_dev(block_table, "block_table", dev, I32, (B, max_pages)), _dev(kv_len, "kv_len", dev, I32, (B,)),
-            None if q_start is None else _dev(q_start, "q_start", dev, I32, (B + 1,)))
-    ws = _workspace(dev, int(lib().cts_kv_attention_workspace_size(ctypes.byref(p), c)) if workspace is None else 0,
-                    workspace)
-    _check(lib().cts_kv_attention(ctypes.byref(p), c, qp, ldq, *args, op, ldo, ws.data_ptr(), ws.numel(),
-                                  _stream(dev)), "cts_kv_attention")
-    return out
+    r = _native.kv_attention(_entry("cts_kv_attention"), _entry("cts_kv_attention_workspace_size"), _raw_stream(dev), dev,
+                             cache._at, q, block_table, kv_len, q_start, max_q, max_kv,
+                             cache.head_dim ** -0.5 if scale is None else scale, window, out, workspace)
+    if r is None:
+        _dt(q, "q")
+        shape = (q.shape[0], q.shape[1], cache.head_dim)
+        _rows(q, "q", dev, q.dtype, shape)
+        if out is not None:
+            _rows(out, "out", dev, q.dtype, shape)
+        B, cols = block_table.shape
+        _dev(block_table, "block_table", dev, I32, (B, cols))
+        _dev(kv_len, "kv_len", dev, I32, (B,))
+        if q_start is not None:
+            _dev(q_start, "q_start", dev, I32, (B + 1,))
+        if workspace is not None:
+            _dev(_binding._workspace(dev, 0, workspace), "workspace", dev, U8)
+        _refused(dev, "kv_attention")
+    _check(r[1], "cts_kv_attention")
+    return r[0]
 
 
 def block_norm(x, weight, y=None, post_weight=None, gate=None, scale=1.0, eps=1e-6, h_out=None, n_out=None):
@@ -142,31 +171,29 @@ def block_norm(x, weight, y=None, post_weight=None, gate=None, scale=1.0, eps=1e
     n = N(h) * weight, N(a) = a / sqrt(mean(a^2) + eps) over a token's elements.
     x, y [T, d]; weights [d]; gate [d] or [T, d].  y None: h is x itself, n its
     norm.  h_out may be x or y.  See cts_block_norm."""
-    dev, (T, d) = x.device, x.shape
-    dt, tdt = _dt(x, "x"), x.dtype
-    xp, ldx = _rows(x, "x", dev, tdt, (T, d))
-    wp = _dev(weight, "weight", dev, tdt, (d,))
-    yp = pp = gp = hp = None
-    ldy = ldg = ldh = 0
-    h = x
-    if y is not None:
-        yp, ldy = _rows(y, "y", dev, tdt, (T, d))
-        if post_weight is not None:
-            pp = _dev(post_weight, "post_weight", dev, tdt, (d,))
+    dev = x.device
+    r = _native.block_norm(_entry("cts_block_norm"), _raw_stream(dev), dev, x, weight, y, post_weight, gate, scale, eps,
+                           h_out, n_out)
+    if r is None:
+        tdt = x.dtype
+        _dt(x, "x")
+        T, d = x.shape
+        if y is None and not (post_weight is None and gate is None and h_out is None):
+            raise ValueError("post_weight, gate and h_out go with y")
+        for t, name in ((x, "x"), (y, "y"), (h_out, "h_out"), (n_out, "n_out")):
+            if t is not None:
+                _rows(t, name, dev, tdt, (T, d))
+        for t, name in ((weight, "weight"), (post_weight, "post_weight")):
+            if t is not None or name == "weight":
+                _dev(t, name, dev, tdt, (d,))
         if gate is not None:
             if gate.dim() == 1:
-                gp = _dev(gate, "gate", dev, tdt, (d,))
+                _dev(gate, "gate", dev, tdt, (d,))
             else:
-                gp, ldg = _rows(gate, "gate", dev, tdt, (T, d))
-        h = torch.empty((T, d), dtype=tdt, device=dev) if h_out is None else h_out
-        hp, ldh = _rows(h, "h_out", dev, tdt, (T, d))
-    elif post_weight is not None or gate is not None or h_out is not None:
-        raise ValueError("post_weight, gate and h_out go with y")
-    n = torch.empty((T, d), dtype=tdt, device=dev) if n_out is None else n_out
-    np_, ldn = _rows(n, "n_out", dev, tdt, (T, d))
-    _check(lib().cts_block_norm(T, d, dt, xp, ldx, yp, ldy, pp, gp, ldg, float(scale), float(eps), wp, hp, ldh, np_, ldn,
-                                _stream(dev)), "cts_block_norm")
-    return h, n
+                _rows(gate, "gate", dev, tdt, (T, d))
+        _refused(dev, "block_norm")
+    _check(r[2], "cts_block_norm")
+    return (x if y is None else r[0]), r[1]
 
 
 def rotary(q, k, cos, sin, positions, sections=None, interleaved=False, q_out=None, k_out=None):
@@ -177,30 +204,29 @@ def rotary(q, k, cos, sin, positions, sections=None, interleaved=False, q_out=No
     some = q if q is not None else k
     if some is None:
         raise ValueError("q or k is needed")
-    dev, tdt, T, d = some.device, some.dtype, some.shape[0], some.shape[2]
-    dt = _dt(some, "q")
-    n_pos, half = cos.shape
-    n_axes = 1 if positions.dim() == 1 else positions.shape[0]
-    args, outs, heads = [], [], []
-    for t, o, name in ((q, q_out, "q"), (k, k_out, "k")):
-        if t is None:
+    dev = some.device
+    r = _native.rotary(_entry("cts_rotary"), _raw_stream(dev), dev, q, k, cos, sin, positions, sections, interleaved, q_out,
+                       k_out)
+    if r is None:
+        tdt = some.dtype
+        _dt(some, "q")
+        T, _, d = some.shape
+        for t, o, name in ((q, q_out, "q"), (k, k_out, "k")):
+            if t is None:
+                if o is not None:
+                    raise ValueError("%s_out goes with %s" % (name, name))
+                continue
+            shape = (T, t.shape[1], d)
+            _rows(t, name, dev, tdt, shape)
             if o is not None:
-                raise ValueError("%s_out goes with %s" % (name, name))
-            args.append((None, 0, None, 0))
-            outs.append(None)
-            heads.append(0)
-            continue
-        shape = (T, t.shape[1], d)
-        o = torch.empty(shape, dtype=tdt, device=dev) if o is None else o
-        args.append(_rows(t, name, dev, tdt, shape) + _rows(o, name + "_out", dev, tdt, shape))
-        outs.append(o)
-        heads.append(t.shape[1])
-    if sections is not None and len(sections) != n_axes:
-        raise ValueError("sections must hold a count for each of the %d axes" % n_axes)
-    sec = None if sections is None else (ctypes.c_int32 * n_axes)(*[int(s) for s in sections])
-    (qp, ldq, qo, ldqo), (kp, ldk, ko, ldko) = args
-    _check(lib().cts_rotary(T, heads[0], heads[1], d, 2 * half, dt, qp, ldq, kp, ldk,
-                            _dev(cos, "cos", dev, F32, (n_pos, half)), _dev(sin, "sin", dev, F32, (n_pos, half)), n_pos,
-                            _dev(positions, "positions", dev, I32, (T,) if positions.dim() == 1 else (n_axes, T)), n_axes,
-                            sec, int(bool(interleaved)), qo, ldqo, ko, ldko, _stream(dev)), "cts_rotary")
-    return outs[0], outs[1]
+                _rows(o, name + "_out", dev, tdt, shape)
+        n_pos, half = cos.shape
+        _dev(cos, "cos", dev, F32, (n_pos, half))
+        _dev(sin, "sin", dev, F32, (n_pos, half))
+        axes = 1 if positions.dim() == 1 else positions.shape[0]
+        _dev(positions, "positions", dev, I32, (T,) if positions.dim() == 1 else (axes, T))
+        if sections is not None and len(sections) != axes:
+            raise ValueError("sections must hold a count for each of the %d axes" % axes)
+        _refused(dev, "rotary")
+    _check(r[2], "cts_rotary")
+    return r[0], r[1]

@@ -1,5 +1,5 @@
 """Builds libcts.so (the HIP kernels and the C ABI) in-tree for gfx950, and
-_marshal.so (the Python binding's tensor checks, host code).
+_marshal.so (the Python binding's tensor checks and calls, host code).
 
     python -m paper_2407_00066_amd.build
 
@@ -54,8 +54,8 @@ def _compile(src: str, build_dir: str = BUILD, sanitize: bool = False) -> str:
 
 
 def build_marshal() -> str:
-    """Compile the binding's tensor checks (csrc/marshal.cpp: host code, torch's
-    C++ API) into _marshal.so."""
+    """Compile the binding's host code (csrc/marshal.cpp, csrc/marshal_block.cpp:
+    torch's C++ API) into _marshal.so."""
     import sysconfig
 
     import torch
@@ -67,10 +67,10 @@ def build_marshal() -> str:
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
            "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI),
            '-DCTS_TORCH_VERSION="%s"' % torch.__version__] + inc + \
-          [os.path.join(CSRC, "marshal.cpp"), "-o", tmp, "-L" + lib, "-ltorch_python", "-ltorch_cpu", "-lc10"]
+          ["-I", INCLUDE, os.path.join(CSRC, "marshal.cpp"), os.path.join(CSRC, "marshal_block.cpp"), "-o", tmp, "-L" + lib, "-ltorch_python", "-ltorch_cpu", "-lc10"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
-        raise RuntimeError("g++ failed on marshal.cpp:\n%s%s" % (r.stdout, r.stderr))
+        raise RuntimeError("g++ failed on marshal.cpp, marshal_block.cpp:\n%s%s" % (r.stdout, r.stderr))
     os.replace(tmp, MARSHAL)
     return MARSHAL
 

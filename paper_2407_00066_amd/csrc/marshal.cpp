@@ -12,6 +12,13 @@
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+// marshal_block.cpp
+PyObject* cts_marshal_kv_write(PyObject*, PyObject* const*, Py_ssize_t);
+PyObject* cts_marshal_kv_read(PyObject*, PyObject* const*, Py_ssize_t);
+PyObject* cts_marshal_kv_attention(PyObject*, PyObject* const*, Py_ssize_t);
+PyObject* cts_marshal_block_norm(PyObject*, PyObject* const*, Py_ssize_t);
+PyObject* cts_marshal_rotary(PyObject*, PyObject* const*, Py_ssize_t);
+
 namespace {
 
 PyObject* address(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -45,9 +52,17 @@ PyObject* address(PyObject*, PyObject* const* args, Py_ssize_t n) {
   }
 }
 
+PyCFunction method(PyObject* (*f)(PyObject*, PyObject* const*, Py_ssize_t)) {
+  return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f));
+}
+
 PyMethodDef methods[] = {
-    {"address", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(address)), METH_FASTCALL,
-     "address(tensor, device, dtype or None, shape or None)"},
+    {"address", method(address), METH_FASTCALL, "address(tensor, device, dtype or None, shape or None)"},
+    {"kv_write", method(cts_marshal_kv_write), METH_FASTCALL, "cts_kv_write, its tensors checked"},
+    {"kv_read", method(cts_marshal_kv_read), METH_FASTCALL, "cts_kv_read, its tensors checked"},
+    {"kv_attention", method(cts_marshal_kv_attention), METH_FASTCALL, "cts_kv_attention, its tensors checked"},
+    {"block_norm", method(cts_marshal_block_norm), METH_FASTCALL, "cts_block_norm, its tensors checked"},
+    {"rotary", method(cts_marshal_rotary), METH_FASTCALL, "cts_rotary, its tensors checked"},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
