@@ -417,8 +417,8 @@ __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(AttnParams p) {
 template <int D, typename TQ, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void attn_tile_kernel(AttnParams p, int large) {
   constexpr int NC = State<D>::NC, NB = State<D>::NB;
-  extern __shared__ float lds[];                   // [WAVES][part_rows][D + 4], then [WAVES][part_rows][2]
-  float* const ml = lds + WAVES * p.part_rows * (D + 4);
+  __shared__ __attribute__((aligned(16))) float sums[WAVES][kRowTile][D + 4];
+  __shared__ float2 ml[WAVES][kRowTile];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int index = blockIdx.x / p.c.heads, h = blockIdx.x - index * p.c.heads;
   Tile t;
@@ -456,7 +456,7 @@ __global__ __launch_bounds__(64 * WAVES) void attn_tile_kernel(AttnParams p, int
     State<D> st;
     attend<D, TQ>(p, t, h, s0, s1, st);
     if (t.row0 + n < t.rows) {
-      float* const o = lds + (wave * p.part_rows + n) * (D + 4);
+      float* const o = sums[wave][n];
 #pragma unroll
       for (int c = 0; c < NC; ++c)
 #pragma unroll
@@ -466,10 +466,10 @@ __global__ __launch_bounds__(64 * WAVES) void attn_tile_kernel(AttnParams p, int
           for (int e = 0; e < NB; ++e) f[e] = st.o[c][e][i];
           store_out<NB>(o + State<D>::element(g, c, i), f);
         }
-      if (g == 0) *reinterpret_cast<float2*>(ml + 2 * (wave * p.part_rows + n)) = make_float2(st.m, st.l);
+      if (g == 0) ml[wave][n] = make_float2(st.m, st.l);
     }
-  } else if (lane < p.part_rows) {                 // fewer steps than waves
-    *reinterpret_cast<float2*>(ml + 2 * (wave * p.part_rows + lane)) = make_float2(-INFINITY, 0.0f);
+  } else if (lane < kRowTile) {                    // fewer steps than waves
+    ml[wave][lane] = make_float2(-INFINITY, 0.0f);
   }
   __syncthreads();
   const int rows = min(kRowTile, t.rows - t.row0);
@@ -477,16 +477,16 @@ __global__ __launch_bounds__(64 * WAVES) void attn_tile_kernel(AttnParams p, int
     const int r = k / (D / 8), e = (k % (D / 8)) * 8;
     float M = -INFINITY;
 #pragma unroll
-    for (int v = 0; v < WAVES; ++v) M = fmaxf(M, ml[2 * (v * p.part_rows + r)]);
+    for (int v = 0; v < WAVES; ++v) M = fmaxf(M, ml[v][r].x);
     const float base = M == -INFINITY ? 0.0f : M;
     float L = 0.0f, f[8] = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
     for (int v = 0; v < WAVES; ++v) {
-      const float2 w = *reinterpret_cast<const float2*>(ml + 2 * (v * p.part_rows + r));
+      const float2 w = ml[v][r];
       if (w.y == 0.0f) continue;                   // saw nothing: no sums
       const float a = __builtin_amdgcn_exp2f(w.x - base);
       L += a * w.y;
-      const float4* o = reinterpret_cast<const float4*>(lds + (v * p.part_rows + r) * (D + 4) + e);
+      const float4* o = reinterpret_cast<const float4*>(&sums[v][r][e]);
       const float4 x = o[0], y = o[1];
       f[0] += a * x.x; f[1] += a * x.y; f[2] += a * x.z; f[3] += a * x.w;
       f[4] += a * y.x; f[5] += a * y.y; f[6] += a * y.z; f[7] += a * y.w;
@@ -500,15 +500,13 @@ __global__ __launch_bounds__(64 * WAVES) void attn_tile_kernel(AttnParams p, int
 
 template <int D, typename TQ, int WAVES>
 void launch_tiles(const AttnParams& p, int64_t tiles, int large, hipStream_t s) {
-  const size_t lds = static_cast<size_t>(WAVES) * p.part_rows * (D + 6) * sizeof(float);
-  attn_tile_kernel<D, TQ, WAVES><<<static_cast<uint32_t>(tiles * p.c.heads), 64 * WAVES, lds, s>>>(p, large);
+  attn_tile_kernel<D, TQ, WAVES><<<static_cast<uint32_t>(tiles * p.c.heads), 64 * WAVES, 0, s>>>(p, large);
 }
 
 template <int D, typename TQ> hipError_t launch(const AttnParams& p, hipStream_t s) {
   const int64_t small = static_cast<int64_t>(p.B) * p.subs;
   if (p.whole) {
-    if (p.whole == 8) launch_tiles<D, TQ, 8>(p, small, 0, s);
-    else launch_tiles<D, TQ, 2>(p, small, 0, s);
+    launch_tiles<D, TQ, 8>(p, small, 0, s);
   } else {
     attn_runs_kernel<D, TQ><<<(p.runs + 3) / 4, 256, 0, s>>>(p);
     attn_join_kernel<D, TQ><<<dim3(static_cast<uint32_t>(small * p.c.heads), p.part_rows), kJoinThreads, 0, s>>>(p);
@@ -540,8 +538,7 @@ bool plan_attention(AttnParams* p, size_t* bytes) {
   // longest sequence does.  Measured at 32 + 8 heads of 128, whole tiles against runs:
   // 1 request of 1024 tokens 8.7 / 10.5 us, of 2048 12.7 / 10.9, of 8192 36 / 14; 8 of 4096
   // 23 / 20; 64 of 4096 60 / 72, of 8192 108 / 121 (of 1000 to 8192 76 / 84).
-  p->whole = span <= 2048 || (span <= 8192 && tiles >= 192) ? 8 : 0;
-  if (p->whole && static_cast<int64_t>(p->part_rows) * (p->c.d + 6) * 32 > 65536) p->whole = 2;
+  p->whole = span <= 2048 || (span <= 8192 && tiles >= 192);
   p->runs = static_cast<int>(std::min<int64_t>(kRuns, (steps + kMinRun - 1) / kMinRun));
   // Few tiles of prompts over many tokens are split along the tokens.  32 + 8 heads of 128,
   // in one piece and so: 128 queries over 4000 tokens 101 / 37 us, 256 over 30000 761 / 170,

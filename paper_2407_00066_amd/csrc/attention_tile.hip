@@ -37,7 +37,7 @@ template <int D> struct Step {
   static constexpr int DB = D / 32;                // row blocks of the second; scale blocks
   static constexpr int KS = D / 16;                // k steps of the first
   static constexpr int KC = D / 8, VC = T / 8;     // 16-byte pieces of a row of keys, of values
-  // Sixteen lanes reading a piece of sixteen rows meet no bank twice (256 bytes wide).
+  // Pieces of 32 rows in turn are read without meeting a bank twice (256 bytes wide).
   static __device__ __forceinline__ int key(int tok, int c) {
     return (tok * KC + (c ^ (KC == 8 ? (tok >> 1) & 7 : tok & 15))) * 16;
   }
@@ -129,35 +129,37 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prompt_kernel
     for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
   float m = -INFINITY, l = 0.0f;
 
-  // what the thread converts: 32 elements of one token's key, and 8 elements of four tokens' values
-  const int k_tok = tid % S::T, k_blk = tid / S::T;
-  const int v_quad = tid % (S::T / 4), v_eighth = tid / (S::T / 4);
-  const int page_mask = (1 << p.c.page_shift) - 1;
+  // What the thread converts, of one group of four tokens: 8 elements of their values,
+  // and 32 of one's key.  Both lie in the same page.
+  const int quad = tid % (S::T / 4), eighth = tid / (S::T / 4);
+  // (which of the four tokens' keys: chosen so that neighbouring lanes write to different banks)
+  const int turn = D == 128 ? (-(quad >> 2)) & 3 : D == 64 ? (quad >> 2) & 3 : 0;
+  const int k_in = (eighth & 3) ^ turn, k_tok = 4 * quad + k_in, k_blk = eighth >> 2;
+  const uint32_t page_mask = (1u << p.c.page_shift) - 1;
+  const uint32_t page_codes = (D / 2) * p.c.heads << p.c.page_shift, head_codes = (D / 2) * h << p.c.page_shift;
+  // (a token's scales lie at a sixteenth of its codes' offset)
+  const uint8_t* const kc = p.c.kc + head_codes + (k_in * (D / 2) + k_blk * 16);
+  const uint8_t* const ks = p.c.ks + head_codes / 16 + (k_in * S::DB + k_blk);
+  const uint8_t* const vc = p.c.vc + head_codes + eighth * 16;
+  const uint8_t* const vs = p.c.vs + head_codes / 16 + (eighth >> 2) * 4;
   const int32_t* const table = p.table + static_cast<int64_t>(b) * p.max_pages;
-  int k_page = 0, v_page = 0;
+  int page = 0;
   uint4 k_raw, v_raw;
   uint32_t k_scale = 0, v_scale = 0;
-  // Tokens past the last seen one read its page's codes or its own; they are masked.
-  auto token = [&](int step, int off) { return min(lo + step * S::T + off, hi - 1); };
-  auto look_up = [&](int step) {
-    k_page = table[token(step, k_tok) >> p.c.page_shift];
-    v_page = table[token(step, 4 * v_quad) >> p.c.page_shift];
-  };
+  // past the last seen token its group stands in, masked
+  auto group = [&](int step) { return min(lo + step * S::T + 4 * quad, (hi - 1) & ~3); };
+  auto look_up = [&](int step) { page = table[group(step) >> p.c.page_shift]; };
   auto load = [&](int step) {
-    {
-      const bool bad = static_cast<uint32_t>(k_page) >= static_cast<uint32_t>(p.c.n_pages);
-      const int64_t at = ((static_cast<int64_t>(bad ? 0 : k_page) * p.c.heads + h) << p.c.page_shift) + (token(step, k_tok) & page_mask);
-      k_raw = *reinterpret_cast<const uint4*>(p.c.kc + at * (D / 2) + k_blk * 16);
-      k_scale = p.c.ks[at * S::DB + k_blk];
-      if (bad) k_scale = 0xffu;
-    }
-    {
-      const bool bad = static_cast<uint32_t>(v_page) >= static_cast<uint32_t>(p.c.n_pages);
-      const int64_t at = ((static_cast<int64_t>(bad ? 0 : v_page) * p.c.heads + h) << p.c.page_shift) +
-                         (token(step, 4 * v_quad) & page_mask & ~3);
-      v_raw = *reinterpret_cast<const uint4*>(p.c.vc + at * (D / 2) + v_eighth * 16);
-      v_scale = *reinterpret_cast<const uint32_t*>(p.c.vs + at * S::DB + (v_eighth >> 2) * 4);
-      if (bad) v_scale = 0xffffffffu;
+    const bool bad = static_cast<uint32_t>(page) >= static_cast<uint32_t>(p.c.n_pages);
+    const uint64_t at = static_cast<uint64_t>(bad ? 0u : static_cast<uint32_t>(page)) * page_codes +
+                        (group(step) & page_mask) * (D / 2);
+    k_raw = *reinterpret_cast<const uint4*>(kc + at);
+    k_scale = ks[at >> 4];
+    v_raw = *reinterpret_cast<const uint4*>(vc + at);
+    v_scale = *reinterpret_cast<const uint32_t*>(vs + (at >> 4));
+    if (bad) {
+      k_scale = 0xffu;
+      v_scale = 0xffffffffu;
     }
   };
   // tokens of a step from here on, or before there, may be hidden from some row of the workgroup
@@ -183,10 +185,10 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prompt_kernel
 #pragma unroll
         for (int j = 0; j < 4; ++j)
           if (((scale >> (8 * j)) & 0xffu) == 0xffu) {
-            const int tok = 4 * v_quad + j;
+            const int tok = 4 * quad + j;
             w[j] = 0;
             scale ^= 0x80u << (8 * j);                                   // 255 -> 127
-            atomicOr(reinterpret_cast<unsigned long long*>(&sh.nan[step % 3][tok >> 6][v_eighth >> 2]), 1ull << (tok & 63));
+            atomicOr(reinterpret_cast<unsigned long long*>(&sh.nan[step % 3][tok >> 6][eighth >> 2]), 1ull << (tok & 63));
           }
       }
       uint32_t y[4][4];
@@ -197,10 +199,10 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prompt_kernel
         for (int e = 0; e < 4; ++e) y[j][e] = fp4_pair(w[j], unit, e);
       }
       // four tokens of one element: half a piece
-      const int piece = (v_quad >> 2) * 2 + (v_quad & 1), half = 8 * ((v_quad >> 1) & 1);
+      const int piece = (quad >> 2) * 2 + (quad & 1), half = 8 * ((quad >> 1) & 1);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int d = 8 * v_eighth + 2 * e;
+        const int d = 8 * eighth + 2 * e;
         *reinterpret_cast<uint2*>(vb + S::value(d, piece) + half) =
             make_uint2(__builtin_amdgcn_perm(y[1][e], y[0][e], 0x05040100u), __builtin_amdgcn_perm(y[3][e], y[2][e], 0x05040100u));
         *reinterpret_cast<uint2*>(vb + S::value(d + 1, piece) + half) =

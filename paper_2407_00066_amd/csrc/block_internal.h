@@ -57,7 +57,7 @@ struct AttnParams {
   // the plan: 16-row tiles of a sequence with few rows, waves its steps are dealt
   // out to, rows of a tile that sums are kept for, tiles of the other sequences
   int subs, runs, part_rows;
-  int whole;                        // waves of a workgroup that takes a whole tile; 0: runs
+  bool whole;                       // a workgroup takes a whole tile, not runs
   int64_t large_tiles;
   float *part, *part_ml;            // [2 runs][part_rows][d] sums, [2 runs][part_rows][2] maxima and lengths
   int32_t* info;                    // [tiles][kv heads][4] a tile's pieces, the first one's slot, its query row, first row and rows
