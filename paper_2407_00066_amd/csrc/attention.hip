@@ -32,9 +32,20 @@ template <int D> struct State {
   }
 };
 
-// The tile's steps [s0, s1) for key/value head h, by one wave.
-template <int D, typename TQ>
-__device__ __forceinline__ void attend(const AttnParams& p, const Tile& t, int h, int s0, int s1, State<D>& st) {
+// Page number of the lane's group of 16 tokens in the steps s0, s0 + stride, ..: two
+// groups a step, a lane one.  Groups past the last seen token are looked up too (what
+// stands there is masked), so that a tile's first look-up need not wait for its length.
+__device__ __forceinline__ int look_up(const AttnParams& p, int b, int lo, int s0, int stride) {
+  const int lane = threadIdx.x & 63;
+  const int tok = lo + (s0 + (lane >> 1) * stride) * kUnit + 16 * (lane & 1);
+  return p.table[static_cast<int64_t>(b) * p.max_pages + min(tok >> p.c.page_shift, p.max_pages - 1)];
+}
+
+// `count` of the tile's steps from s0, `stride` apart, for key/value head h, by one
+// wave; pages: look_up of the first 32.
+template <int D, typename TQ, int stride>
+__device__ __forceinline__ void attend(const AttnParams& p, const Tile& t, int h, int s0, int count, int pages,
+                                       State<D>& st) {
   constexpr int NS = sizeof(TQ) == 4 ? 3 : 1;
   constexpr int KS = D / 32;                     // steps of the first product; words of keys a lane holds
   constexpr int NC = State<D>::NC, NB = State<D>::NB;
@@ -72,21 +83,11 @@ __device__ __forceinline__ void attend(const AttnParams& p, const Tile& t, int h
   const int all_hi = t.first_pos + t.row0 / p.group + 1;
   const int all_lo = p.window ? t.first_pos + (min(t.rows, t.row0 + kRowTile) - 1) / p.group - p.window + 1 : 0;
 
-  // Page numbers of the next 32 steps, two groups of 16 tokens each, a lane one:
-  // a step's addresses do not wait for its own look-up.  A group past the last
-  // seen token is not looked up: the last group's codes stand in for it, masked.
-  const int last16 = (t.hi - 1) & ~15;
-  int pages = 0;
-  auto look_up = [&](int s) {
-    const int tok = min(t.lo + s * kUnit + 16 * lane, last16);
-    pages = p.table[static_cast<int64_t>(t.b) * p.max_pages + (tok >> p.c.page_shift)];
-  };
-  // token offset of a group's first token within the cache's heads, and whether its page is outside the cache
-  struct Group { int64_t base; bool bad; };
+  struct Group { int64_t base; bool bad; };           // a group's first token among its head's, its page outside the cache
   const int page_mask = (1 << p.c.page_shift) - 1;
-  auto group_of = [&](int s, int i) -> Group {
-    const int page = __builtin_amdgcn_readlane(pages, 2 * ((s - s0) & 31) + i);
-    const int tok = min(t.lo + s * kUnit + 16 * i, last16);
+  auto group_of = [&](int it, int i) -> Group {
+    const int page = __builtin_amdgcn_readlane(pages, 2 * (it & 31) + i);
+    const int tok = t.lo + (s0 + it * stride) * kUnit + 16 * i;
     const bool bad = static_cast<uint32_t>(page) >= static_cast<uint32_t>(p.c.n_pages);
     return {((static_cast<int64_t>(bad ? 0 : page) * p.c.heads + h) << p.c.page_shift) + (tok & page_mask), bad};
   };
@@ -101,10 +102,10 @@ __device__ __forceinline__ void attend(const AttnParams& p, const Tile& t, int h
   uint32_t k[2][KS], ks[2], vs[2][NC];
   uint4 v[2][NC];
   Group gr[2];
-  auto load_k = [&](int s) {
+  auto load_k = [&](int it) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      gr[i] = group_of(s, i);
+      gr[i] = group_of(it, i);
       const uint8_t* kc = p.c.kc + gr[i].base * (D / 2);
       const uint8_t* sc = p.c.ks + gr[i].base * (D / 32);
       if constexpr (D == 64) {
@@ -135,11 +136,10 @@ __device__ __forceinline__ void attend(const AttnParams& p, const Tile& t, int h
     }
   };
 
-  look_up(s0);
-  load_k(s0);
+  load_k(0);
   load_v();
-  for (int s = s0; s < s1; ++s) {
-    const int at = t.lo + s * kUnit;
+  for (int it = 0; it < count; ++it) {
+    const int at = t.lo + (s0 + it * stride) * kUnit;
     // scores of the lane's row against tokens at + 16 i + 4 g + j
     f32x4 x[2];
 #pragma unroll
@@ -156,8 +156,8 @@ __device__ __forceinline__ void attend(const AttnParams& p, const Tile& t, int h
     }
     // the next keys are on their way during the softmax and the second product,
     // the next values during the next first product (past the end: the last step's again)
-    const int next = min(s + 1, s1 - 1);
-    if (((next - s0) & 31) == 0 && next != s0) look_up(next);
+    const int next = min(it + 1, count - 1);
+    if ((next & 31) == 0 && next != 0) pages = look_up(p, t.b, t.lo, s0 + next * stride, stride);
     load_k(next);
 
     float sc[8];
@@ -312,7 +312,7 @@ __global__ __launch_bounds__(256, D == 256 || sizeof(TQ) == 4 ? 2 : 4) void attn
   for (int u = u0; u < u1;) {
     const int steps = min(t.steps - step, u1 - u);
     State<D> st;
-    attend<D, TQ>(p, t, h, step, step + steps, st);
+    attend<D, TQ, 1>(p, t, h, step, steps, look_up(p, t.b, t.lo, step, 1), st);
     const bool whole = steps == t.steps;
     const int slot = 2 * w + (u == u0 ? 0 : 1);
     if (t.row0 + n < t.rows) {
@@ -421,6 +421,9 @@ __global__ __launch_bounds__(64 * WAVES) void attn_tile_kernel(AttnParams p, int
   __shared__ float2 ml[WAVES][kRowTile];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int index = blockIdx.x / p.c.heads, h = blockIdx.x - index * p.c.heads;
+  // the waves take steps in turn: their first pages are on their way while the tile's length is
+  int pages = 0;
+  if (!large && !p.window) pages = look_up(p, index / p.subs, 0, wave, WAVES);
   Tile t;
   if (large) {
     int b = -1, sub = 0;
@@ -450,11 +453,11 @@ __global__ __launch_bounds__(64 * WAVES) void attn_tile_kernel(AttnParams p, int
     t = uniform(small_tile(p, index));
   }
   if (t.steps == 0) return;
-  const int s0 = t.steps * wave / WAVES, s1 = t.steps * (wave + 1) / WAVES;
   const int n = lane & 15, g = lane >> 4;
-  if (s0 < s1) {
+  if (wave < t.steps) {
     State<D> st;
-    attend<D, TQ>(p, t, h, s0, s1, st);
+    if (large || p.window) pages = look_up(p, t.b, t.lo, wave, WAVES);
+    attend<D, TQ, WAVES>(p, t, h, wave, (t.steps - wave + WAVES - 1) / WAVES, pages, st);
     if (t.row0 + n < t.rows) {
       float* const o = sums[wave][n];
 #pragma unroll
