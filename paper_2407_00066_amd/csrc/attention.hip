@@ -46,6 +46,9 @@ __device__ __forceinline__ int look_up(const AttnParams& p, int b, int lo, int s
 template <int D, typename TQ, int stride>
 __device__ __forceinline__ void attend(const AttnParams& p, const Tile& t, int h, int s0, int count, int pages,
                                        State<D>& st) {
+  // Parts of a query (bf16: itself) and of a weight.  bf16 weights are rounded once:
+  // a second part brings the error against 64 bits from 1.25 to 1.0 times that of rounding
+  // the output alone, and takes 41 -> 52 us for 64 requests of 40 to 4000 tokens.
   constexpr int NS = sizeof(TQ) == 4 ? 3 : 1;
   constexpr int KS = D / 32;                     // steps of the first product; words of keys a lane holds
   constexpr int NC = State<D>::NC, NB = State<D>::NB;
@@ -190,10 +193,14 @@ __device__ __forceinline__ void attend(const AttnParams& p, const Tile& t, int h
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       w[i] = __builtin_amdgcn_exp2f(sc[i] - base);
-      st.l += w[i];
+      if (NS == 3) st.l += w[i];
     }
     bf16x8 pf[NS];
     split<NS>(w, pf);
+    if (NS == 1) {
+      const uint4 x = __builtin_bit_cast(uint4, pf[0]);
+      st.l = add_pair(x.x, add_pair(x.y, add_pair(x.z, add_pair(x.w, st.l))));
+    }
 
 #pragma unroll
     for (int c = 0; c < NC; ++c) {

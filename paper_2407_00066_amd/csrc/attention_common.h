@@ -67,6 +67,14 @@ __device__ __forceinline__ bf16x8 frag(uint32_t a, uint32_t b, uint32_t c, uint3
   return __builtin_bit_cast(bf16x8, v);
 }
 
+// l + both halves of a pair of bf16 weights.  A row's length is the sum of its weights as
+// they are multiplied: where one token has most of the weight, the weight's rounding
+// then cancels.
+__device__ __forceinline__ float add_pair(uint32_t w, float l) {
+  typedef short short2_ __attribute__((ext_vector_type(2)));
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(short2_, w), __builtin_bit_cast(short2_, 0x3f803f80u), l, false);
+}
+
 // eight floats as NS bf16 parts whose sum is the float (to 8, 16 or 24 bits)
 template <int NS> __device__ __forceinline__ void split(const float* f, bf16x8* out) {
   float r[8];
