@@ -73,8 +73,9 @@ int cts_kv_read(const cts_kv_cache* c, int32_t T, const int64_t* slots, void* k,
  * [T][n_q_heads][head_dim] of dtype, rows ldq and ldo apart.
  * Arithmetic: scores, softmax and sums in fp32.  Cached elements are exact in
  * bf16 (bf16 matrix cores).  bf16: the weights w are rounded to bf16 for the
- * product with v (2^-8 each at most, the size of the output's own rounding); f32: queries
- * and weights are split into three bf16 parts, which keep their 24 bits.
+ * product with v, and their sum is that of the rounded ones (2^-8 each at most, the size
+ * of the output's own rounding); f32: queries and weights are split into three
+ * bf16 parts, which keep their 24 bits.
  * What is masked is never read into a result, NaN included.
  * max_q and max_kv bound the queries of a sequence and kv_len; tokens past
  * max_kv and queries past max_q are left out (out keeps what it held there).

@@ -14,7 +14,7 @@ import ctypes
 import torch
 
 from . import _binding
-from ._binding import AttnProblem, KvCacheArrays, _check, _check_tensor, _dev, _dt, _load_marshal, _stream, lib
+from ._binding import AttnProblem, KvCacheArrays, _check, _check_tensor, _dev, _dt, _load_marshal, lib
 
 U8, I32, I64, F32 = torch.uint8, torch.int32, torch.int64, torch.float32
 
@@ -33,7 +33,8 @@ def _entry(name: str) -> int:
 
 
 def _raw_stream(device: torch.device) -> int:
-    return _stream(device) if device.type == "cuda" else 0
+    # (a tensor's device has an index)
+    return torch._C._cuda_getCurrentRawStream(device.index) if device.type == "cuda" else 0
 
 
 def _refused(device: torch.device, where: str):

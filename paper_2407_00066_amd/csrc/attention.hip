@@ -523,7 +523,7 @@ template <int D, typename TQ> hipError_t launch(const AttnParams& p, hipStream_t
   }
   if (static_cast<int64_t>(p.max_q) * p.group > kSmallRows) {
     if constexpr (sizeof(TQ) == 2) return launch_attention_prompts(p, s);
-    launch_tiles<D, TQ, D == 256 ? 2 : 4>(p, p.large_tiles, 1, s);
+    else launch_tiles<D, TQ, D == 256 ? 2 : 4>(p, p.large_tiles, 1, s);
   }
   return hipGetLastError();
 }
