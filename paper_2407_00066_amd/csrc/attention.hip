@@ -281,37 +281,39 @@ __global__ __launch_bounds__(256, D == 256 || sizeof(TQ) == 4 ? 2 : 4) void attn
   const int lane = threadIdx.x & 63, tiles = p.B * p.subs;
   const int w = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
   int4* const info = reinterpret_cast<int4*>(p.info);
-  int mine = 0;
-  for (int i = lane; i < tiles; i += 64) {
-    const int steps = small_tile(p, i).steps;
-    if (steps == 0 && i % p.runs == w)
+  // the lanes count the steps of 64 tiles at a time (a head's); the first 64 are kept
+  int n0 = 0, to0 = 0, total = 0;
+  for (int base = 0; base < tiles; base += 64) {
+    const int i = base + lane, steps = i < tiles ? small_tile(p, i).steps : 0;
+    if (i < tiles && steps == 0 && i % p.runs == w)
       for (int h = 0; h < p.c.heads; ++h) info[static_cast<int64_t>(i) * p.c.heads + h] = make_int4(0, 0, 0, 0);
-    mine += steps;
+    const int to = wave_scan(steps);
+    if (base == 0) {
+      n0 = steps;
+      to0 = to;
+    }
+    total += __builtin_amdgcn_readlane(to, 63);
   }
-#pragma unroll
-  for (int k = 1; k < 64; k <<= 1) mine += __shfl_xor(mine, k);
-  const int total = __builtin_amdgcn_readfirstlane(mine) * p.c.heads;
+  total *= p.c.heads;
   if (total == 0) return;
-  // a run of kMinRun steps at least; the first `more` runs are one longer
-  const int runs = min(p.runs, (total + kMinRun - 1) / kMinRun);
+  // the first `more` runs are one longer
+  const int runs = static_cast<int>(runs_of(total));
   if (w >= runs) return;
   const int len = total / runs, more = total - len * runs;
   const int u0 = w * len + min(w, more), u1 = u0 + len + (w < more ? 1 : 0);
   // the tile that holds step u0, and that tile's first step
   int index = 0, start = 0;
   for (int base = 0, before = 0; base < tiles; base += 64) {
-    const int n = base + lane < tiles ? small_tile(p, base + lane).steps * p.c.heads : 0;
-    int to = n;
-#pragma unroll
-    for (int k = 1; k < 64; k <<= 1) {
-      const int up = __shfl_up(to, k);
-      if (lane >= k) to += up;
+    int n = n0, to = to0;
+    if (base) {
+      n = base + lane < tiles ? small_tile(p, base + lane).steps : 0;
+      to = wave_scan(n);
     }
-    const uint64_t here = __ballot(before + to > u0);                   // the first such lane's tile
+    const uint64_t here = __ballot((before + to) * p.c.heads > u0);     // the first such lane's tile
     if (here) {
       const int first = __builtin_ctzll(here);
       index = base + first;
-      start = before + __builtin_amdgcn_readlane(to - n, first);
+      start = (before + __builtin_amdgcn_readlane(to - n, first)) * p.c.heads;
       break;
     }
     before += __builtin_amdgcn_readlane(to, 63);
@@ -443,12 +445,7 @@ __global__ __launch_bounds__(64 * WAVES) void attn_tile_kernel(AttnParams p, int
         const int rows = min(queries_of(p, base + lane).n, p.max_q) * p.group;
         n = rows > kSmallRows ? (rows + kRowTile - 1) / kRowTile : 0;
       }
-      int to = n;
-#pragma unroll
-      for (int k = 1; k < 64; k <<= 1) {
-        const int up = __shfl_up(to, k);
-        if (lane >= k) to += up;
-      }
+      const int to = wave_scan(n);
       const uint64_t here = __ballot(before + to > index);
       if (here) {
         const int at = __builtin_ctzll(here);
@@ -552,7 +549,7 @@ bool plan_attention(AttnParams* p, size_t* bytes) {
   // 1 request of 1024 tokens 8.7 / 10.5 us, of 2048 12.7 / 10.9, of 8192 36 / 14; 8 of 4096
   // 23 / 20; 64 of 4096 60 / 72, of 8192 108 / 121 (of 1000 to 8192 76 / 84).
   p->whole = span <= 2048 || (span <= 8192 && tiles >= 192);
-  p->runs = static_cast<int>(std::min<int64_t>(kRuns, (steps + kMinRun - 1) / kMinRun));
+  p->runs = static_cast<int>(runs_of(steps));
   // Few tiles of prompts over many tokens are split along the tokens.  32 + 8 heads of 128,
   // in one piece and so: 128 queries over 4000 tokens 101 / 37 us, 256 over 30000 761 / 170,
   // 512 over themselves 21 / 21 (24 with pieces of four steps).

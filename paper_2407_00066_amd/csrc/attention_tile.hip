@@ -65,12 +65,7 @@ __device__ __forceinline__ bool find_tile(const AttnParams& p, int index, int* b
       const int rows = min(queries_of(p, base + lane).n, p.max_q) * p.group;
       count = rows > kSmallRows ? (rows + kRows - 1) / kRows : 0;
     }
-    int to = count;
-#pragma unroll
-    for (int k = 1; k < 64; k <<= 1) {
-      const int up = __shfl_up(to, k);
-      if (lane >= k) to += up;
-    }
+    const int to = wave_scan(count);
     const uint64_t here = __ballot(before + to > index);
     if (here) {
       const int at = __builtin_ctzll(here);
