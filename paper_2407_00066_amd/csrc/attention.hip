@@ -275,6 +275,9 @@ __device__ __forceinline__ TQ* out_at(const AttnParams& p, const Tile& t, int h,
 // differ.  A run starts and ends inside a tile as a rule: those two leave their
 // sums in the workspace (slots 2 w and 2 w + 1) for the join, the tiles between
 // are whole and final.
+// Few tiles: each counts as a whole number of runs, so that no wave takes two
+// pieces one after the other (8 heads of 128, one request of 2500 tokens 11.4 / 10.0 us,
+// two of 5001 15.5 / 14.4).
 template <int D, typename TQ>
 __global__ __launch_bounds__(256, D == 256 || sizeof(TQ) == 4 ? 2 : 4) void attn_runs_kernel(AttnParams p) {
   constexpr int NC = State<D>::NC, NB = State<D>::NB;
@@ -296,30 +299,45 @@ __global__ __launch_bounds__(256, D == 256 || sizeof(TQ) == 4 ? 2 : 4) void attn
   }
   total *= p.c.heads;
   if (total == 0) return;
-  // the first `more` runs are one longer
-  const int runs = static_cast<int>(runs_of(total));
+  int runs, len, more = 0;                            // the first `more` runs are one longer
+  const bool few = tiles * p.c.heads <= kFewTiles && total <= kFewSteps;
+  const int shift = few ? (total > 2048 ? 2 : 1) : 0, round = (1 << shift) - 1;
+  if (few) {
+    total = 0;
+    for (int base = 0; base < tiles; base += 64) {
+      const int n = base ? (base + lane < tiles ? small_tile(p, base + lane).steps : 0) : n0;
+      const int to = wave_scan((n + round) >> shift);
+      if (base == 0) to0 = to;
+      total += __builtin_amdgcn_readlane(to, 63);
+    }
+    runs = total * p.c.heads;
+    len = 1 << shift;
+  } else {
+    runs = min(kRuns, (total + 3) / 4);
+    len = total / runs;
+    more = total - len * runs;
+  }
   if (w >= runs) return;
-  const int len = total / runs, more = total - len * runs;
   const int u0 = w * len + min(w, more), u1 = u0 + len + (w < more ? 1 : 0);
   // the tile that holds step u0, and that tile's first step
   int index = 0, start = 0;
   for (int base = 0, before = 0; base < tiles; base += 64) {
     int n = n0, to = to0;
-    if (base) {
-      n = base + lane < tiles ? small_tile(p, base + lane).steps : 0;
-      to = wave_scan(n);
-    }
-    const uint64_t here = __ballot((before + to) * p.c.heads > u0);     // the first such lane's tile
+    if (base) n = base + lane < tiles ? small_tile(p, base + lane).steps : 0;
+    n = (n + round) >> shift;
+    if (base) to = wave_scan(n);
+    const uint64_t here = __ballot(((before + to) * p.c.heads << shift) > u0);     // the first such lane's tile
     if (here) {
       const int first = __builtin_ctzll(here);
       index = base + first;
-      start = (before + __builtin_amdgcn_readlane(to - n, first)) * p.c.heads;
+      start = (before + __builtin_amdgcn_readlane(to - n, first)) * p.c.heads << shift;
       break;
     }
     before += __builtin_amdgcn_readlane(to, 63);
   }
   Tile t = uniform(small_tile(p, index));
-  int h = (u0 - start) / t.steps, step = u0 - start - h * t.steps;
+  int all = (t.steps + round) & ~round;                                 // what the tile counts as
+  int h = (u0 - start) / all, step = u0 - start - h * all;
   const int n = lane & 15, g = lane >> 4;
   for (int u = u0; u < u1;) {
     const int steps = min(t.steps - step, u1 - u);
@@ -357,15 +375,17 @@ __global__ __launch_bounds__(256, D == 256 || sizeof(TQ) == 4 ? 2 : 4) void attn
     }
     if (step == 0 && lane == 0) {
       // the tile starts here; its pieces end in the run that holds its last step
-      const int last = u + t.steps - 1, cut = (len + 1) * more;
+      const int last = u + all - 1, cut = (len + 1) * more;
       const int to = last < cut ? last / (len + 1) : more + (last - cut) / len;
       info[static_cast<int64_t>(index) * p.c.heads + h] = make_int4(to - w + 1, slot, t.q0, t.row0 << 8 | min(kRowTile, t.rows - t.row0));
     }
     u += steps;
     step = 0;
+    if (few) break;
     if (u < u1 && ++h == p.c.heads) {
       h = 0;
       do t = uniform(small_tile(p, ++index)); while (t.steps == 0);
+      all = t.steps;
     }
   }
 }
@@ -542,14 +562,15 @@ bool plan_attention(AttnParams* p, size_t* bytes) {
   if (p->window) span = std::min<int64_t>(span, static_cast<int64_t>(p->window) + kRowTile + kUnit);
   const int64_t tiles = static_cast<int64_t>(p->B) * p->subs * p->c.heads;
   if (tiles > 0x7fffffff || p->large_tiles * p->c.heads > 0x7fffffff) return false;
-  const int64_t steps = tiles * std::max<int64_t>(1, (span + kUnit - 1) / kUnit);
+  const int64_t most_steps = std::max<int64_t>(1, (span + kUnit - 1) / kUnit), steps = tiles * most_steps;
   if (steps > 0x7fffffff) return false;
   // A tile's steps shared by one workgroup's waves need no join, but last as long as the
   // longest sequence does.  Measured at 32 + 8 heads of 128, whole tiles against runs:
   // 1 request of 1024 tokens 8.7 / 10.5 us, of 2048 12.7 / 10.9, of 8192 36 / 14; 8 of 4096
   // 23 / 20; 64 of 4096 60 / 72, of 8192 108 / 121 (of 1000 to 8192 76 / 84).
   p->whole = span <= 2048 || (span <= 8192 && tiles >= 192);
-  p->runs = static_cast<int>(runs_of(steps));
+  // what the kernel makes at most: of few tiles, each a whole number of runs of two steps or more
+  p->runs = static_cast<int>(std::min<int64_t>(kRuns, tiles * ((most_steps + 1) / 2)));
   // Few tiles of prompts over many tokens are split along the tokens.  32 + 8 heads of 128,
   // in one piece and so: 128 queries over 4000 tokens 101 / 37 us, 256 over 30000 761 / 170,
   // 512 over themselves 21 / 21 (24 with pieces of four steps).

@@ -10,13 +10,8 @@ constexpr int kRowTile = 16;       // query rows of a tile
 constexpr int kUnit = 32;          // tokens of a step
 constexpr int kSmallRows = 64;     // rows of a sequence that the 16-row tiles are for
 constexpr int kRuns = 4096;        // waves that a batch's steps are dealt out to: 16 for every compute unit
-// Runs that `steps` steps are dealt out as: four steps each at least, two where that
-// makes no more than 1024 (one request of 8192 tokens, 8 heads of 128: 13.8 us with four, 12.8 so).
-__host__ __device__ inline int64_t runs_of(int64_t steps) {
-  const int64_t four = (steps + 3) / 4, two = (steps + 1) / 2, some = two < 1024 ? two : 1024;
-  const int64_t n = four > some ? four : some;
-  return n < kRuns ? n : kRuns;
-}
+constexpr int kFewTiles = 256;     // tiles (x heads) and steps up to which each tile is cut into runs
+constexpr int kFewSteps = 4 * (kRuns - kFewTiles);   // of its own: no more than kRuns of four steps
 constexpr int kJoinThreads = 256;
 constexpr int kPromptRows = 128;   // query rows of a workgroup for prompts
 constexpr int64_t kPromptGroups = 512;  // workgroups that few prompts are split into: two for every compute unit
