@@ -89,13 +89,13 @@ __device__ __forceinline__ void attend(const AttnParams& p, const Tile& t, int h
   const int all_hi = t.first_pos + t.row0 / p.group + 1;
   const int all_lo = p.window ? t.first_pos + (min(t.rows, t.row0 + kRowTile) - 1) / p.group - p.window + 1 : 0;
 
-  struct Group { int64_t base; bool bad; };           // a group's first token among its head's, its page outside the cache
+  struct Group { int64_t base; uint32_t bad; };       // a group's first token among its head's; all ones: its page is outside the cache
   const int page_mask = (1 << p.c.page_shift) - 1;
   auto group_of = [&](int it, int i) -> Group {
     const int page = __builtin_amdgcn_readlane(pages, 2 * (it & 31) + i);
     const int tok = t.lo + (s0 + it * stride) * kUnit + 16 * i;
     const bool bad = static_cast<uint32_t>(page) >= static_cast<uint32_t>(p.c.n_pages);
-    return {((static_cast<int64_t>(bad ? 0 : page) * p.c.heads + h) << p.c.page_shift) + (tok & page_mask), bad};
+    return {((static_cast<int64_t>(bad ? 0 : page) * p.c.heads + h) << p.c.page_shift) + (tok & page_mask), bad ? ~0u : 0u};
   };
   const uint32_t k_at = n * (D / 2) + g * (D / 8), ks_at = n * (D / 32) + (D == 64 ? g >> 1 : D == 128 ? g : 2 * g);
   uint32_t v_at[NC], vs_at[NC];
@@ -105,7 +105,7 @@ __device__ __forceinline__ void attend(const AttnParams& p, const Tile& t, int h
     v_at[c] = (g * (D / 8) + eighth) * 16;
     vs_at[c] = (g * (D / 32) + eighth / 4) * 4;
   }
-  uint32_t k[2][KS], ks[2], vs[2][NC];
+  uint32_t k[2][KS], ks[2], vs[2][NC], v_bad[2];
   uint4 v[2][NC];
   Group gr[2];
   auto load_k = [&](int it) {
@@ -125,7 +125,6 @@ __device__ __forceinline__ void attend(const AttnParams& p, const Tile& t, int h
         }
       }
       ks[i] = D == 256 ? *reinterpret_cast<const uint16_t*>(sc + ks_at) : sc[ks_at];
-      if (gr[i].bad) ks[i] = 0xffffu;
     }
   };
   auto load_v = [&]() {                                                  // of the step load_k was last called for
@@ -137,8 +136,8 @@ __device__ __forceinline__ void attend(const AttnParams& p, const Tile& t, int h
       for (int c = 0; c < NC; ++c) {
         v[i][c] = *reinterpret_cast<const uint4*>(vc + v_at[c]);
         vs[i][c] = *reinterpret_cast<const uint32_t*>(sc + vs_at[c]);
-        if (gr[i].bad) vs[i][c] = 0xffffffffu;
       }
+      v_bad[i] = gr[i].bad;
     }
   };
 
@@ -151,9 +150,10 @@ __device__ __forceinline__ void attend(const AttnParams& p, const Tile& t, int h
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       x[i] = f32x4{0, 0, 0, 0};
+      const uint32_t units = ks[i] | gr[i].bad;                          // here: asked for sooner, it would be waited for sooner
 #pragma unroll
       for (int y = 0; y < KS; ++y) {
-        const float unit = unit_of(ks[i], D == 256 ? y / 4 : 0);
+        const float unit = unit_of(units, D == 256 ? y / 4 : 0);
         const bf16x8 a = frag(fp4_pair(k[i][y], unit, 0), fp4_pair(k[i][y], unit, 1),
                               fp4_pair(k[i][y], unit, 2), fp4_pair(k[i][y], unit, 3));
 #pragma unroll
@@ -163,7 +163,7 @@ __device__ __forceinline__ void attend(const AttnParams& p, const Tile& t, int h
     // the next keys are on their way during the softmax and the second product,
     // the next values during the next first product (past the end: the last step's again)
     const int next = min(it + 1, count - 1);
-    if ((next & 31) == 0 && next != 0) pages = look_up(p, t.b, t.lo, s0 + next * stride, stride);
+    if ((next & 31) == 0 && next != 0) pages = rare(look_up(p, t.b, t.lo, s0 + next * stride, stride));
     load_k(next);
 
     float sc[8];
@@ -207,6 +207,8 @@ __device__ __forceinline__ void attend(const AttnParams& p, const Tile& t, int h
 
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
+      vs[0][c] |= v_bad[0];
+      vs[1][c] |= v_bad[1];
       if (masked) {
         // A weight of zero does not hide a NaN value: NaN blocks are taken out of
         // the product, and the rows that do see one are made NaN.
