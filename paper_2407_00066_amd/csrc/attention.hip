@@ -272,25 +272,93 @@ __device__ __forceinline__ TQ* out_at(const AttnParams& p, const Tile& t, int h,
   return static_cast<TQ*>(p.out) + (t.q0 + query) * p.ldo + static_cast<int64_t>(h * p.group + row - query * p.group) * D;
 }
 
-// The batch's steps (of the sequences with few rows), tile after tile and head
-// after head, are dealt out to the waves in equal runs, however the lengths
-// differ.  A run starts and ends inside a tile as a rule: those two leave their
-// sums in the workspace (slots 2 w and 2 w + 1) for the join, the tiles between
-// are whole and final.
-// Few tiles: each counts as a whole number of runs, so that no wave takes two
-// pieces one after the other (8 heads of 128, one request of 2500 tokens 11.4 / 10.0 us,
-// two of 5001 15.5 / 14.4).
+// What WAVES waves of a workgroup have of the same rows, in shared memory.
+template <int D, int WAVES> struct Shared {
+  float sums[WAVES][kRowTile][D + 4];
+  float2 ml[WAVES][kRowTile];
+};
+
+// The wave's steps (every WAVES-th of `steps` from s0, its own first) into shared memory.
+template <int D, typename TQ, int WAVES>
+__device__ __forceinline__ void attend_shared(const AttnParams& p, const Tile& t, int h, int s0, int steps, int wave,
+                                              int pages, Shared<D, WAVES>& sh) {
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  if (wave < steps) {
+    State<D> st;
+    attend<D, TQ, WAVES>(p, t, h, s0 + wave, (steps - wave + WAVES - 1) / WAVES, pages, st);
+    if (t.row0 + n < t.rows) {
+      float* const o = sh.sums[wave][n];
+#pragma unroll
+      for (int c = 0; c < State<D>::NC; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float f[State<D>::NB];
+#pragma unroll
+          for (int e = 0; e < State<D>::NB; ++e) f[e] = st.o[c][e][i];
+          store_out<State<D>::NB>(o + State<D>::element(g, c, i), f);
+        }
+      if (g == 0) sh.ml[wave][n] = make_float2(st.m, st.l);
+    }
+  } else if (lane < kRowTile) {                    // fewer steps than waves
+    sh.ml[wave][lane] = make_float2(-INFINITY, 0.0f);
+  }
+}
+
+// Eight elements of a row, from e: the waves' sums together, their maximum and length.
+template <int D, int WAVES>
+__device__ __forceinline__ float2 join_waves(const Shared<D, WAVES>& sh, int r, int e, float* f) {
+  float M = -INFINITY;
+#pragma unroll
+  for (int v = 0; v < WAVES; ++v) M = fmaxf(M, sh.ml[v][r].x);
+  const float base = M == -INFINITY ? 0.0f : M;
+  float L = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = 0.0f;
+#pragma unroll
+  for (int v = 0; v < WAVES; ++v) {
+    const float2 w = sh.ml[v][r];
+    if (w.y == 0.0f) continue;                     // saw nothing: no sums
+    const float a = __builtin_amdgcn_exp2f(w.x - base);
+    L += a * w.y;
+    const float4* o = reinterpret_cast<const float4*>(&sh.sums[v][r][e]);
+    const float4 x = o[0], y = o[1];
+    f[0] += a * x.x; f[1] += a * x.y; f[2] += a * x.z; f[3] += a * x.w;
+    f[4] += a * y.x; f[5] += a * y.y; f[6] += a * y.z; f[7] += a * y.w;
+  }
+  return make_float2(M, L);
+}
+
 template <int D, typename TQ>
-__global__ __launch_bounds__(256, D == 256 || sizeof(TQ) == 4 ? 2 : 4) void attn_runs_kernel(AttnParams p) {
-  constexpr int NC = State<D>::NC, NB = State<D>::NB;
-  const int lane = threadIdx.x & 63, tiles = p.B * p.subs;
-  const int w = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+__device__ __forceinline__ void put_row(const AttnParams& p, const Tile& t, int h, int r, int e, float L, float* f) {
+  const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] *= inv;
+  store_out<8>(out_at<D, TQ>(p, t, h, r) + e, f);
+}
+
+// The batch's steps (of the sequences with few rows), tile after tile and head
+// after head, are dealt out to the workgroups in equal runs, however the lengths
+// differ; a run's waves take its steps in turn and join in shared memory (a wave with
+// a run of its own leaves eight times the sums to the join: 32 requests of 30000 tokens,
+// 32 + 8 heads of 128, 213 / 203 us).  A run starts and ends inside a tile as a rule:
+// those two leave their sums in the workspace (slots 2 w and 2 w + 1) for the join,
+// the tiles between are whole and final.
+// Few tiles are each cut into a whole number of runs, so that no workgroup takes two
+// pieces one after the other (one request of 131072 tokens 38.2 / 37.3 us, of 40000
+// 20.6 / 17.2).  One workgroup for every compute unit: two, 1 request of 18000 tokens
+// 16.0 / 14.6, 4 of 100000 95 / 90.  Heads of 64 leave too few bytes under way so, and
+// have two (one of 200000 tokens 37.9 / 36.0); of heads of 256 a compute unit holds one.
+template <int D, typename TQ>
+__global__ __launch_bounds__(64 * kWaves, D == 256 || sizeof(TQ) == 4 ? 2 : 4) void attn_runs_kernel(AttnParams p) {
+  __shared__ __attribute__((aligned(16))) Shared<D, kWaves> sh;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int tiles = p.B * p.subs, w = blockIdx.x;
   int4* const info = reinterpret_cast<int4*>(p.info);
   // the lanes count the steps of 64 tiles at a time (a head's); the first 64 are kept
   int n0 = 0, to0 = 0, total = 0;
   for (int base = 0; base < tiles; base += 64) {
     const int i = base + lane, steps = i < tiles ? small_tile(p, i).steps : 0;
-    if (i < tiles && steps == 0 && i % p.runs == w)
+    if (i < tiles && steps == 0 && i % p.runs == w && wave == 0)
       for (int h = 0; h < p.c.heads; ++h) info[static_cast<int64_t>(i) * p.c.heads + h] = make_int4(0, 0, 0, 0);
     const int to = wave_scan(steps);
     if (base == 0) {
@@ -302,20 +370,27 @@ __global__ __launch_bounds__(256, D == 256 || sizeof(TQ) == 4 ? 2 : 4) void attn
   total *= p.c.heads;
   if (total == 0) return;
   int runs, len, more = 0;                            // the first `more` runs are one longer
-  const bool few = tiles * p.c.heads <= kFewTiles && total <= kFewSteps;
-  const int shift = few ? (total > 2048 ? 2 : 1) : 0, round = (1 << shift) - 1;
+  const bool few = tiles * p.c.heads <= kFewTiles;
+  auto pieces = [&](int n) {                          // runs of a tile, or its steps
+    if (!few) return n;
+    return len == kWaves ? (n + kWaves - 1) / kWaves : (n + len - 1) / len;        // few steps: no division
+  };
   if (few) {
-    total = 0;
-    for (int base = 0; base < tiles; base += 64) {
-      const int n = base ? (base + lane < tiles ? small_tile(p, base + lane).steps : 0) : n0;
-      const int to = wave_scan((n + round) >> shift);
-      if (base == 0) to0 = to;
-      total += __builtin_amdgcn_readlane(to, 63);
+    // as long as the most workgroups allow, a sixteenth longer until their number is kept to
+    constexpr int kMost = D == 64 ? kRuns : kRuns / 2;
+    len = ((total - 1) / (kMost * kWaves) + 1) * kWaves;
+    for (;;) {
+      runs = 0;
+      for (int base = 0; base < tiles; base += 64) {
+        const int to = wave_scan(pieces(base ? (base + lane < tiles ? small_tile(p, base + lane).steps : 0) : n0));
+        if (base == 0) to0 = to;
+        runs += __builtin_amdgcn_readlane(to, 63) * p.c.heads;
+      }
+      if (runs <= kMost) break;
+      len += (len / (16 * kWaves) + 1) * kWaves;
     }
-    runs = total * p.c.heads;
-    len = 1 << shift;
   } else {
-    runs = min(kRuns, (total + 3) / 4);
+    runs = min(D == 256 ? kRuns / 2 : kRuns, (total + kWaves - 1) / kWaves);
     len = total / runs;
     more = total - len * runs;
   }
@@ -326,56 +401,38 @@ __global__ __launch_bounds__(256, D == 256 || sizeof(TQ) == 4 ? 2 : 4) void attn
   for (int base = 0, before = 0; base < tiles; base += 64) {
     int n = n0, to = to0;
     if (base) n = base + lane < tiles ? small_tile(p, base + lane).steps : 0;
-    n = (n + round) >> shift;
+    n = pieces(n);
     if (base) to = wave_scan(n);
-    const uint64_t here = __ballot(((before + to) * p.c.heads << shift) > u0);     // the first such lane's tile
+    const uint64_t here = __ballot((before + to) * p.c.heads > (few ? w : u0));    // the first such lane's tile
     if (here) {
       const int first = __builtin_ctzll(here);
       index = base + first;
-      start = (before + __builtin_amdgcn_readlane(to - n, first)) * p.c.heads << shift;
+      start = (before + __builtin_amdgcn_readlane(to - n, first)) * p.c.heads * (few ? len : 1);
       break;
     }
     before += __builtin_amdgcn_readlane(to, 63);
   }
   Tile t = uniform(small_tile(p, index));
-  int all = (t.steps + round) & ~round;                                 // what the tile counts as
+  int all = few ? pieces(t.steps) * len : t.steps;                       // what the tile counts as
   int h = (u0 - start) / all, step = u0 - start - h * all;
-  const int n = lane & 15, g = lane >> 4;
   for (int u = u0; u < u1;) {
     const int steps = min(t.steps - step, u1 - u);
-    State<D> st;
-    attend<D, TQ, 1>(p, t, h, step, steps, look_up(p, t.b, t.lo, step, 1), st);
-    const bool whole = steps == t.steps;
+    attend_shared<D, TQ, kWaves>(p, t, h, step, steps, wave, look_up(p, t.b, t.lo, step + wave, kWaves), sh);
+    __syncthreads();
     const int slot = 2 * w + (u == u0 ? 0 : 1);
-    if (t.row0 + n < t.rows) {
-      if (whole) {
-        const float inv = st.l == 0.0f ? 0.0f : 1.0f / st.l;
-        TQ* const o = out_at<D, TQ>(p, t, h, n);
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float f[NB];
-#pragma unroll
-            for (int e = 0; e < NB; ++e) f[e] = st.o[c][e][i] * inv;
-            store_out<NB>(o + State<D>::element(g, c, i), f);
-          }
+    for (int k = threadIdx.x; k < min(kRowTile, t.rows - t.row0) * (D / 8); k += 64 * kWaves) {
+      const int r = k / (D / 8), e = (k % (D / 8)) * 8;
+      float f[8];
+      const float2 ml = join_waves<D, kWaves>(sh, r, e, f);
+      if (steps == t.steps) {
+        put_row<D, TQ>(p, t, h, r, e, ml.y, f);
       } else {
-        const int64_t at = static_cast<int64_t>(slot) * p.part_rows + n;
-        float* const o = p.part + at * D;
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float f[NB];
-#pragma unroll
-            for (int e = 0; e < NB; ++e) f[e] = st.o[c][e][i];
-            store_out<NB>(o + State<D>::element(g, c, i), f);
-          }
-        if (g == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * at) = make_float2(st.m, st.l);
+        const int64_t at = static_cast<int64_t>(slot) * p.part_rows + r;
+        store_out<8>(p.part + at * D + e, f);
+        if (e == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * at) = ml;
       }
     }
-    if (step == 0 && lane == 0) {
+    if (step == 0 && threadIdx.x == 0) {
       // the tile starts here; its pieces end in the run that holds its last step
       const int last = u + all - 1, cut = (len + 1) * more;
       const int to = last < cut ? last / (len + 1) : more + (last - cut) / len;
@@ -383,12 +440,13 @@ __global__ __launch_bounds__(256, D == 256 || sizeof(TQ) == 4 ? 2 : 4) void attn
     }
     u += steps;
     step = 0;
-    if (few) break;
-    if (u < u1 && ++h == p.c.heads) {
+    if (few || u >= u1) break;
+    if (++h == p.c.heads) {
       h = 0;
       do t = uniform(small_tile(p, ++index)); while (t.steps == 0);
       all = t.steps;
     }
+    __syncthreads();
   }
 }
 
@@ -450,9 +508,7 @@ __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(AttnParams p) {
 // found by counting them (their number is known on the device only).
 template <int D, typename TQ, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void attn_tile_kernel(AttnParams p, int large) {
-  constexpr int NC = State<D>::NC, NB = State<D>::NB;
-  __shared__ __attribute__((aligned(16))) float sums[WAVES][kRowTile][D + 4];
-  __shared__ float2 ml[WAVES][kRowTile];
+  __shared__ __attribute__((aligned(16))) Shared<D, WAVES> sh;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int index = blockIdx.x / p.c.heads, h = blockIdx.x - index * p.c.heads;
   // the waves take steps in turn: their first pages are on their way while the tile's length is
@@ -482,51 +538,14 @@ __global__ __launch_bounds__(64 * WAVES) void attn_tile_kernel(AttnParams p, int
     t = uniform(small_tile(p, index));
   }
   if (t.steps == 0) return;
-  const int n = lane & 15, g = lane >> 4;
-  if (wave < t.steps) {
-    State<D> st;
-    if (large || p.window) pages = look_up(p, t.b, t.lo, wave, WAVES);
-    attend<D, TQ, WAVES>(p, t, h, wave, (t.steps - wave + WAVES - 1) / WAVES, pages, st);
-    if (t.row0 + n < t.rows) {
-      float* const o = sums[wave][n];
-#pragma unroll
-      for (int c = 0; c < NC; ++c)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float f[NB];
-#pragma unroll
-          for (int e = 0; e < NB; ++e) f[e] = st.o[c][e][i];
-          store_out<NB>(o + State<D>::element(g, c, i), f);
-        }
-      if (g == 0) ml[wave][n] = make_float2(st.m, st.l);
-    }
-  } else if (lane < kRowTile) {                    // fewer steps than waves
-    ml[wave][lane] = make_float2(-INFINITY, 0.0f);
-  }
+  if (large || p.window) pages = look_up(p, t.b, t.lo, wave, WAVES);
+  attend_shared<D, TQ, WAVES>(p, t, h, 0, t.steps, wave, pages, sh);
   __syncthreads();
-  const int rows = min(kRowTile, t.rows - t.row0);
-  for (int k = threadIdx.x; k < rows * (D / 8); k += 64 * WAVES) {
+  for (int k = threadIdx.x; k < min(kRowTile, t.rows - t.row0) * (D / 8); k += 64 * WAVES) {
     const int r = k / (D / 8), e = (k % (D / 8)) * 8;
-    float M = -INFINITY;
-#pragma unroll
-    for (int v = 0; v < WAVES; ++v) M = fmaxf(M, ml[v][r].x);
-    const float base = M == -INFINITY ? 0.0f : M;
-    float L = 0.0f, f[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-#pragma unroll
-    for (int v = 0; v < WAVES; ++v) {
-      const float2 w = ml[v][r];
-      if (w.y == 0.0f) continue;                   // saw nothing: no sums
-      const float a = __builtin_amdgcn_exp2f(w.x - base);
-      L += a * w.y;
-      const float4* o = reinterpret_cast<const float4*>(&sums[v][r][e]);
-      const float4 x = o[0], y = o[1];
-      f[0] += a * x.x; f[1] += a * x.y; f[2] += a * x.z; f[3] += a * x.w;
-      f[4] += a * y.x; f[5] += a * y.y; f[6] += a * y.z; f[7] += a * y.w;
-    }
-    const float inv = L == 0.0f ? 0.0f : 1.0f / L;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] *= inv;
-    store_out<8>(out_at<D, TQ>(p, t, h, r) + e, f);
+    float f[8];
+    const float L = join_waves<D, WAVES>(sh, r, e, f).y;
+    put_row<D, TQ>(p, t, h, r, e, L, f);
   }
 }
 
@@ -538,9 +557,9 @@ void launch_tiles(const AttnParams& p, int64_t tiles, int large, hipStream_t s) 
 template <int D, typename TQ> hipError_t launch(const AttnParams& p, hipStream_t s) {
   const int64_t small = static_cast<int64_t>(p.B) * p.subs;
   if (p.whole) {
-    launch_tiles<D, TQ, 8>(p, small, 0, s);
+    launch_tiles<D, TQ, kWaves>(p, small, 0, s);
   } else {
-    attn_runs_kernel<D, TQ><<<(p.runs + 3) / 4, 256, 0, s>>>(p);
+    attn_runs_kernel<D, TQ><<<p.runs, 64 * kWaves, 0, s>>>(p);
     attn_join_kernel<D, TQ><<<dim3(static_cast<uint32_t>(small * p.c.heads), p.part_rows), kJoinThreads, 0, s>>>(p);
   }
   if (static_cast<int64_t>(p.max_q) * p.group > kSmallRows) {
@@ -565,14 +584,15 @@ bool plan_attention(AttnParams* p, size_t* bytes) {
   const int64_t tiles = static_cast<int64_t>(p->B) * p->subs * p->c.heads;
   if (tiles > 0x7fffffff || p->large_tiles * p->c.heads > 0x7fffffff) return false;
   const int64_t most_steps = std::max<int64_t>(1, (span + kUnit - 1) / kUnit), steps = tiles * most_steps;
-  if (steps > 0x7fffffff) return false;
-  // A tile's steps shared by one workgroup's waves need no join, but last as long as the
-  // longest sequence does.  Measured at 32 + 8 heads of 128, whole tiles against runs:
-  // 1 request of 1024 tokens 8.7 / 10.5 us, of 2048 12.7 / 10.9, of 8192 36 / 14; 8 of 4096
-  // 23 / 20; 64 of 4096 60 / 72, of 8192 108 / 121 (of 1000 to 8192 76 / 84).
-  p->whole = span <= 2048 || (span <= 8192 && tiles >= 192);
-  // what the kernel makes at most: of few tiles, each a whole number of runs of two steps or more
-  p->runs = static_cast<int>(std::min<int64_t>(kRuns, tiles * ((most_steps + 1) / 2)));
+  if (steps > 0x50000000) return false;               // counted in 32 bits, rounded up to runs by less than a half
+  // A tile's steps taken by one workgroup need no join, but last as long as the longest
+  // sequence does.  Measured at 32 + 8 heads of 128, whole tiles against runs: 1 request of
+  // 1024 tokens 8.5 / 10.3 us, of 2048 12.4 / 10.0; 8 of 2000 13.3 / 13.4, of 4000 21 / 16;
+  // 16 of 4000 21 / 25, of 8000 44 / 39; 64 of 4000 56 / 63, of 8000 106 / 114 (of 1000 to
+  // 8000 78 / 83); 24 of 8000 46 / 54 (of 1000 to 8000 40 / 33).
+  p->whole = span <= std::min<int64_t>(8192, 1024 + 16 * tiles);
+  // what the kernel makes at most, of a step or more for each wave
+  p->runs = static_cast<int>(std::min<int64_t>(kRuns, tiles * ((most_steps + kWaves - 1) / kWaves)));
   // Few tiles of prompts over many tokens are split along the tokens.  32 + 8 heads of 128,
   // in one piece and so: 128 queries over 4000 tokens 101 / 37 us, 256 over 30000 761 / 170,
   // 512 over themselves 21 / 21 (24 with pieces of four steps).

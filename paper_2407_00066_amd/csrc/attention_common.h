@@ -9,9 +9,9 @@ namespace {
 constexpr int kRowTile = 16;       // query rows of a tile
 constexpr int kUnit = 32;          // tokens of a step
 constexpr int kSmallRows = 64;     // rows of a sequence that the 16-row tiles are for
-constexpr int kRuns = 4096;        // waves that a batch's steps are dealt out to: 16 for every compute unit
-constexpr int kFewTiles = 256;     // tiles (x heads) and steps up to which each tile is cut into runs
-constexpr int kFewSteps = 4 * (kRuns - kFewTiles);   // of its own: no more than kRuns of four steps
+constexpr int kWaves = 8;          // waves of a workgroup that share a tile's steps
+constexpr int kRuns = 512;         // runs of steps, at most: two workgroups for every compute unit
+constexpr int kFewTiles = 64;      // tiles (x heads) up to which each tile is cut into runs of its own
 constexpr int kJoinThreads = 256;
 constexpr int kPromptRows = 128;   // query rows of a workgroup for prompts
 constexpr int64_t kPromptGroups = 512;  // workgroups that few prompts are split into: two for every compute unit
