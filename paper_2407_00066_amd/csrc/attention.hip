@@ -355,7 +355,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 || sizeof(TQ) == 4 ? 2 : 4) v
   const int tiles = p.B * p.subs, w = blockIdx.x;
   int4* const info = reinterpret_cast<int4*>(p.info);
   // the lanes count the steps of 64 tiles at a time (a head's); the first 64 are kept
-  int n0 = 0, to0 = 0, total = 0;
+  int n0 = 0, to0 = 0, total = 0, some = 0;           // some: tiles that have any
   for (int base = 0; base < tiles; base += 64) {
     const int i = base + lane, steps = i < tiles ? small_tile(p, i).steps : 0;
     if (i < tiles && steps == 0 && i % p.runs == w && wave == 0)
@@ -366,11 +366,12 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 || sizeof(TQ) == 4 ? 2 : 4) v
       to0 = to;
     }
     total += __builtin_amdgcn_readlane(to, 63);
+    some += __builtin_popcountll(__ballot(steps > 0));
   }
   total *= p.c.heads;
   if (total == 0) return;
   int runs, len, more = 0;                            // the first `more` runs are one longer
-  const bool few = tiles * p.c.heads <= kFewTiles;
+  const bool few = some * p.c.heads <= kFewTiles;
   auto pieces = [&](int n) {                          // runs of a tile, or its steps
     if (!few) return n;
     return len == kWaves ? (n + kWaves - 1) / kWaves : (n + len - 1) / len;        // few steps: no division
@@ -588,9 +589,9 @@ bool plan_attention(AttnParams* p, size_t* bytes) {
   // A tile's steps taken by one workgroup need no join, but last as long as the longest
   // sequence does.  Measured at 32 + 8 heads of 128, whole tiles against runs: 1 request of
   // 1024 tokens 8.5 / 10.3 us, of 2048 12.4 / 10.0; 8 of 2000 13.3 / 13.4, of 4000 21 / 16;
-  // 16 of 4000 21 / 25, of 8000 44 / 39; 64 of 4000 56 / 63, of 8000 106 / 114 (of 1000 to
-  // 8000 78 / 83); 24 of 8000 46 / 54 (of 1000 to 8000 40 / 33).
-  p->whole = span <= std::min<int64_t>(8192, 1024 + 16 * tiles);
+  // 24 of 4000 34 / 39, of 8000 46 / 54 (of 1000 to 8000 40 / 33); 32 of 8000 56 / 66 (45 / 47);
+  // 64 of 8000 106 / 114 (78 / 83), of 16000 205 / 212 (147 / 140).
+  p->whole = span <= (tiles >= 256 ? 8192 : 1024 + 16 * tiles);
   // what the kernel makes at most, of a step or more for each wave
   p->runs = static_cast<int>(std::min<int64_t>(kRuns, tiles * ((most_steps + kWaves - 1) / kWaves)));
   // Few tiles of prompts over many tokens are split along the tokens.  32 + 8 heads of 128,
