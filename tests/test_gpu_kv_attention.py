@@ -105,6 +105,28 @@ def test_long_sequences_in_pieces():
     check(make([1, 1], [1700, 900], 2, 2, 256, 16, "f32", seed=10))
 
 
+# a bound far above the lengths: the steps are dealt out over the whole card, runs begin and
+# end inside sequences, cover several of them, or a few sequences are cut into pieces
+@pytest.mark.parametrize("window", [0, 45])
+@pytest.mark.parametrize("d,dtype", [(64, "bf16"), (128, "bf16"), (256, "bf16"), (128, "f32"), (64, "f32")])
+@pytest.mark.parametrize("B,kvh,top", [(3, 2, 2600), (7, 3, 1500), (90, 1, 300), (40, 4, 700), (1, 1, 4000)])
+def test_equal_runs(B, kvh, top, d, dtype, window):
+    rng = np.random.default_rng(B + d)
+    n_kv = rng.integers(1, top, B)
+    n_kv[0], n_kv[-1], n_kv[B // 2] = top, max(1, top - 77), 3 if B > 1 else top
+    n_q = np.minimum(rng.integers(1, 4, B), n_kv)
+    if B > 4:                                                        # nothing cached, no rows, many rows
+        n_kv[2], n_q[3], n_q[4], n_kv[4] = 0, 0, 40, 200
+    check(make(n_q.tolist(), n_kv.tolist(), 2 * kvh, kvh, d, 16, dtype, seed=B + d), window=window, max_kv=10 ** 6)
+
+
+def test_more_steps_than_runs_of_one():
+    """Runs of several steps a wave, of unequal sequences; heads that leave a compute unit idle."""
+    check(make([1, 1, 1], [20011, 9000, 33], 5, 5, 64, 32, seed=15))
+    check(make([2, 1], [17000, 31], 3, 1, 128, 64, seed=16))
+    check(make([1] * 66, [130 * i + 7 for i in range(66)], 1, 1, 128, 16, seed=17), max_kv=10 ** 6)
+
+
 def test_max_kv_and_wider_tables():
     """max_kv only has to bound the lengths: a loose and a tight one, and a wider table, agree with the oracle."""
     c = make([1, 2], [333, 200], 8, 2, 128, 16, seed=12)
