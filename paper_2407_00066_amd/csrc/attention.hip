@@ -11,9 +11,9 @@
 //   queries are loaded in the same order); result: row = token 4 g + i, column n =
 //   query row.  Second: A row = element, k = tokens 4 g .. 4 g + 3 of two groups of 16.
 // Codes become bf16 in registers, two an instruction with their scale; nothing is
-// staged in shared memory.  Bound by the cache's bytes where there are many (64 requests of 4096
-// tokens: 57 us, 5.0 TB/s; four of 40000 to 131072: 85 us, 4.3 TB/s), by the chain of length,
-// page, codes and join where there are few (one of 709 tokens: 7.6 us).
+// staged in shared memory.  Bound by the cache's bytes where there are many (64 requests of 4000
+// tokens: 57 us, 4.9 TB/s; four of 40000 to 131072: 78 us, 4.7 TB/s), by the chain of length,
+// page, codes and join where there are few (one of 709 tokens: 7.7 us).
 #include <algorithm>
 
 #include "attention_common.h"
@@ -511,7 +511,29 @@ template <int D, typename TQ, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void attn_tile_kernel(AttnParams p, int large) {
   __shared__ __attribute__((aligned(16))) Shared<D, WAVES> sh;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int index = blockIdx.x / p.c.heads, h = blockIdx.x - index * p.c.heads;
+  int index = blockIdx.x / p.c.heads;
+  const int h = blockIdx.x - index * p.c.heads, tiles = p.B * p.subs * p.c.heads;
+  if (!large && tiles > 256 && tiles <= 512 && p.B <= 128 && p.max_kv >= 1024) {
+    // Up to two workgroups for every compute unit: the longest sequences go first, and the
+    // second workgroups take the others the other way round.  The waves look for the sequence
+    // of that rank, each among its share of them.  32 + 8 heads of 128: 64 requests of 40 to
+    // 4000 tokens 41 / 33.5 us, of 1000 to 8000 79 / 66; 64 of 4000 each 57.2 / 58.6, of 300
+    // 9.8 / 10.8.  Where there are more workgroups they start as others end, and the order
+    // (longest first) matters less than what it takes: 128 of 4000 107.5 / 110, of 500 to 4000 68.9 / 67.6.
+    __shared__ int found;
+    const int b = index / p.subs, first = 256 / (p.subs * p.c.heads);
+    const int want = b < first ? b : p.B - 1 - (b - first);
+    auto key_of = [&](int i) -> uint32_t {             // by length, then as they come; no two alike
+      return i < p.B ? min(max(p.kv_len[i], 0), 1 << 28) / kUnit << 7 | (127 - i) : 0;
+    };
+    const uint32_t low = key_of(lane), high = key_of(lane + 64);
+    for (int i = wave; i < p.B; i += WAVES) {
+      const uint32_t mine = __builtin_amdgcn_readlane(i < 64 ? low : high, i & 63);
+      if (__builtin_popcountll(__ballot(low > mine)) + __builtin_popcountll(__ballot(high > mine)) == want) found = i;
+    }
+    __syncthreads();
+    index += (__builtin_amdgcn_readfirstlane(found) - b) * p.subs;
+  }
   // the waves take steps in turn: their first pages are on their way while the tile's length is
   int pages = 0;
   if (!large && !p.window) pages = look_up(p, index / p.subs, 0, wave, WAVES);
@@ -590,7 +612,7 @@ bool plan_attention(AttnParams* p, size_t* bytes) {
   // sequence does.  Measured at 32 + 8 heads of 128, whole tiles against runs: 1 request of
   // 1024 tokens 8.5 / 10.3 us, of 2048 12.4 / 10.0; 8 of 2000 13.3 / 13.4, of 4000 21 / 16;
   // 24 of 4000 34 / 39, of 8000 46 / 54 (of 1000 to 8000 40 / 33); 32 of 8000 56 / 66 (45 / 47);
-  // 64 of 8000 106 / 114 (78 / 83), of 16000 205 / 212 (147 / 140).
+  // 64 of 8000 106 / 114 (66 / 83).
   p->whole = span <= (tiles >= 256 ? 8192 : 1024 + 16 * tiles);
   // what the kernel makes at most, of a step or more for each wave
   p->runs = static_cast<int>(std::min<int64_t>(kRuns, tiles * ((most_steps + kWaves - 1) / kWaves)));

@@ -120,6 +120,19 @@ def test_equal_runs(B, kvh, top, d, dtype, window):
     check(make(n_q.tolist(), n_kv.tolist(), 2 * kvh, kvh, d, 16, dtype, seed=B + d), window=window, max_kv=10 ** 6)
 
 
+# one to two workgroups for every compute unit: they take the sequences in the order of their lengths
+@pytest.mark.parametrize("B,kvh,d", [(64, 8, 64), (33, 8, 128), (65, 4, 64), (128, 3, 64), (2, 200, 64), (40, 12, 64), (1, 300, 64), (128, 4, 64)])
+def test_sequences_in_order_of_length(B, kvh, d):
+    rng = np.random.default_rng(B)
+    n_kv = rng.integers(0, 150, B)
+    n_kv[1::5] = 64                                                  # equal ones among them
+    check(make([1] * B, n_kv.tolist(), kvh, kvh, d, 16, seed=B), max_kv=2000)
+    n_q = np.minimum(rng.integers(0, 4, B), n_kv)
+    check(make(n_q.tolist(), n_kv.tolist(), 9 * kvh, kvh, d, 16, seed=B + 1), max_kv=2000)
+    n_kv[:] = 1
+    check(make([1] * B, n_kv.tolist(), kvh, kvh, d, 16, seed=B + 2), max_kv=2000)
+
+
 def test_more_steps_than_runs_of_one():
     """Runs of several steps a wave, of unequal sequences; heads that leave a compute unit idle."""
     check(make([1, 1, 1], [20011, 9000, 33], 5, 5, 64, 32, seed=15))
