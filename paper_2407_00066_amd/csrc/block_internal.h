@@ -54,7 +54,7 @@ struct AttnParams {
   int T, B, heads, group;           // group: query heads of a key/value head
   int max_pages, max_q, max_kv, window, dtype;
   float scale_log2e;
-  // the plan: 16-row tiles of a sequence with few rows, waves its steps are dealt
+  // the plan: 16-row tiles of a sequence with few rows, workgroups its steps are dealt
   // out to, rows of a tile that sums are kept for, tiles of the other sequences
   int subs, runs, part_rows;
   bool whole;                       // a workgroup takes a whole tile, not runs
