@@ -29,7 +29,9 @@ extern "C" {
  * 1024), n_heads key/value heads of head_dim (64, 128 or 256) elements.
  * Each 32 elements along head_dim share a scale byte s; an element is a 4-bit
  * code, bit 3 the sign and the rest the magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6,
- * standing for magnitude x 2^(s - 127) (a microscaled 4-bit float).  Bytes:
+ * standing for magnitude x 2^(s - 127) (a microscaled 4-bit float), s at most 252; a
+ * block with s == 255 is NaN throughout.  253 and 254 are no scales of a token that
+ * is read (some of their magnitudes lie past the largest float).  Bytes:
  *   k_codes  [n_pages][n_heads][page_size][head_dim / 2]        element 2i in byte i's low half
  *   k_scales [n_pages][n_heads][page_size][head_dim / 32]
  *   v_codes  [n_pages][n_heads][page_size / 4][head_dim / 8][4][4]   8 elements of 4 tokens in 16 bytes
@@ -76,7 +78,8 @@ int cts_kv_read(const cts_kv_cache* c, int32_t T, const int64_t* slots, void* k,
  * product with v, and their sum is that of the rounded ones (2^-8 each at most, the size
  * of the output's own rounding); f32: queries and weights are split into three
  * bf16 parts, which keep their 24 bits.
- * What is masked is never read into a result, NaN included.
+ * What is masked is never read into a result, whatever bytes stand there, NaN and
+ * scales of 253 and 254 included.
  * max_q and max_kv bound the queries of a sequence and kv_len; tokens past
  * max_kv and queries past max_q are left out (out keeps what it held there).
  * They choose how the work is split and size the workspace.  A page number

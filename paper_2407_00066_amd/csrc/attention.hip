@@ -210,14 +210,14 @@ __device__ __forceinline__ void attend(const AttnParams& p, const Tile& t, int h
       vs[0][c] |= v_bad[0];
       vs[1][c] |= v_bad[1];
       if (masked) {
-        // A weight of zero does not hide a NaN value: NaN blocks are taken out of
-        // the product, and the rows that do see one are made NaN.
+        // A weight of zero does not hide a NaN or infinite value: blocks that can hold one are
+        // taken out of the product, and the rows that do see one are made NaN.
         uint32_t hit[4] = {0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            if (((rare(static_cast<int>(vs[i][c])) >> (8 * j)) & 0xff) == 0xff) hit[2 * i + j / 2] |= 0x3f80u << (16 * (j & 1));
+            if (past_scales(rare(static_cast<int>(vs[i][c])), j)) hit[2 * i + j / 2] |= 0x3f80u << (16 * (j & 1));
         if (__any((hit[0] | hit[1] | hit[2] | hit[3]) != 0)) {
           float in[8];
 #pragma unroll
@@ -225,7 +225,7 @@ __device__ __forceinline__ void attend(const AttnParams& p, const Tile& t, int h
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
               in[4 * i + j] = seen(at + 4 * g, i, j) ? 1.0f : 0.0f;
-              if (((vs[i][c] >> (8 * j)) & 0xffu) == 0xffu) {
+              if (past_scales(vs[i][c], j)) {
                 vs[i][c] ^= 0x80u << (8 * j);                            // 255 -> 127
                 (&v[i][c].x)[j] = 0;
               }

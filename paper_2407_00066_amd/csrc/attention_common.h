@@ -40,6 +40,9 @@ __device__ __forceinline__ int rare(int v) {
 #endif
   return v;
 }
+// Whether byte i of w is past the scales that are written (at most 252): 255, a NaN
+// block, or 253 and 254, which put some magnitudes past the largest float.
+__device__ __forceinline__ bool past_scales(uint32_t w, int i) { return ((w >> (8 * i)) & 0xffu) > 252u; }
 // the float 2^(s - 127) of byte i of w (255: as the conversion's NaN scale)
 __device__ __forceinline__ float unit_of(uint32_t w, int i) {
   return __uint_as_float((i < 3 ? w << (23 - 8 * i) : w >> 1) & 0x7f800000u);

@@ -184,11 +184,11 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prompt_kernel
       uint32_t scale = v_scale;
       const int at = lo + step * S::T;
       if (at + S::T > wg_all_hi || at < wg_all_lo) {
-        // A weight of zero does not hide a NaN: where rows may be masked, NaN
-        // blocks are taken out and noted, and the rows that see them made NaN.
+        // A weight of zero does not hide a NaN or an infinity: where rows may be masked, blocks
+        // that can hold one are taken out and noted, and the rows that see them made NaN.
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          if (((scale >> (8 * j)) & 0xffu) == 0xffu) {
+          if (past_scales(scale, j)) {
             const int tok = 4 * quad + j;
             w[j] = 0;
             scale ^= 0x80u << (8 * j);                                   // 255 -> 127
