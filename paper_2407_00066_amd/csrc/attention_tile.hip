@@ -294,7 +294,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prompt_kernel
         const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[mb][2 * i], p.scale_log2e, -base));
         const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[mb][2 * i + 1], p.scale_log2e, -base));
         w[i] = f32_to_bf16_pair(x, y);
-        l += x + y;
+        l = add_pair(w[i], l);
       }
       pf[mb][0] = frag(w[0], w[1], w[2], w[3]);
       pf[mb][1] = frag(w[4], w[5], w[6], w[7]);
