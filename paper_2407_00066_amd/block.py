@@ -138,13 +138,16 @@ def kv_attention_workspace_size(q, cache: KVCache, B, max_q, max_kv, window=0) -
     return int(lib().cts_kv_attention_workspace_size(ctypes.byref(p), ctypes.byref(cache._c)))
 
 
-def kv_attention(q, cache: KVCache, block_table, kv_len, q_start=None, max_q=1, max_kv=None, scale=None, window=0,
+def kv_attention(q, cache: KVCache, block_table, kv_len, q_start=None, max_q=None, max_kv=None, scale=None, window=0,
                  out=None, workspace=None):
     """Causal attention of q [T, n_q_heads, head_dim] over the cached tokens of
     the sequences of block_table [B, max_pages] and kv_len [B] (int32); q_start
     [B + 1] (int32) gives each sequence's query rows, None one row each.  max_q
-    and max_kv bound the queries of a sequence and kv_len (max_kv None: what the
-    table has room for).  scale None: head_dim^-1/2.  See cts_kv_attention."""
+    and max_kv bound the queries of a sequence and kv_len (None: all rows of q, and
+    what the table has room for; tight bounds choose faster kernels).  Rows that
+    belong to no sequence, or lie past max_q in theirs, are not written: without
+    `out` they hold whatever the new tensor's memory did.  scale None:
+    head_dim^-1/2.  See cts_kv_attention."""
     dev = cache.device
     r = _native.kv_attention(_entry("cts_kv_attention"), _entry("cts_kv_attention_workspace_size"), _raw_stream(dev), dev,
                              cache._at, q, block_table, kv_len, q_start, max_q, max_kv,
