@@ -4,16 +4,19 @@
 // address, torch's current stream and the Python call's arguments, checks the
 // tensors, allocates what the caller did not give, and makes the call.  It returns
 // the outputs with the call's status, or None if an argument is not as it has to
-// be: the Python side then finds out what is wrong and says so.
+// be: the Python side then finds out what is wrong and says so.  An allocation that
+// fails raises torch's own error for it.
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <torch/csrc/Device.h>
 #include <torch/csrc/Dtype.h>
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <algorithm>
+#include <exception>
 #include <optional>
 
 #include "cts_block.h"
@@ -24,6 +27,21 @@ namespace {
 struct Refused {};
 void need(bool ok) {
   if (!ok) throw Refused{};
+}
+
+// What an allocation that failed ends a call with.
+struct Failed { std::exception_ptr why; };
+at::Tensor allocate(at::IntArrayRef shape, c10::ScalarType dt, c10::Device dev) {
+  try {
+    return at::empty(shape, at::TensorOptions().dtype(dt).device(dev));
+  } catch (...) {
+    throw Failed{std::current_exception()};
+  }
+}
+PyObject* raise(const Failed& f) {
+  HANDLE_TH_ERRORS
+  std::rethrow_exception(f.why);
+  END_HANDLE_TH_ERRORS
 }
 
 const at::Tensor& tensor(PyObject* o) {
@@ -84,8 +102,7 @@ Rows rows(const at::Tensor& t, c10::Device dev, c10::ScalarType dt, at::IntArray
 }
 
 at::Tensor fresh(PyObject* given, at::IntArrayRef shape, c10::ScalarType dt, c10::Device dev) {
-  if (given != Py_None) return tensor(given);
-  return at::empty(shape, at::TensorOptions().dtype(dt).device(dev));
+  return given != Py_None ? tensor(given) : allocate(shape, dt, dev);
 }
 
 c10::Device device_of(PyObject* o) {
@@ -101,7 +118,8 @@ const cts_kv_cache& cache_of(PyObject* o) {
 
 PyObject* wrap(const at::Tensor& t) { return THPVariable_Wrap(t); }
 
-// Runs f; None for a refusal and for tensors that only stand for others.
+// Runs f; None for a refusal, and for tensors whose sizes or storage cannot be had (they
+// only stand for others, or raise errors of their own, which come again with Python's checks).
 template <typename F> PyObject* call(Py_ssize_t n, Py_ssize_t want, F f) {
   if (n != want) {
     PyErr_Format(PyExc_TypeError, "%zd arguments, expected %zd", n, want);
@@ -110,9 +128,8 @@ template <typename F> PyObject* call(Py_ssize_t n, Py_ssize_t want, F f) {
   try {
     return f();
   } catch (const Refused&) {
-  } catch (const c10::OutOfMemoryError& e) {
-    PyErr_SetString(PyExc_RuntimeError, e.what_without_backtrace());
-    return nullptr;
+  } catch (const Failed& f) {
+    return raise(f);
   } catch (const std::exception&) {
   }
   PyErr_Clear();
@@ -191,7 +208,7 @@ PyObject* cts_marshal_kv_attention(PyObject*, PyObject* const* a, Py_ssize_t n) 
       need(ws.device() == dev && ws.scalar_type() == at::kByte && ws.is_contiguous());
     } else {
       const int64_t bytes = entry<decltype(&cts_kv_attention_workspace_size)>(a[1])(&p, &c);
-      ws = at::empty({bytes > 0 ? bytes : 1}, at::TensorOptions().dtype(at::kByte).device(dev));
+      ws = allocate({bytes > 0 ? bytes : 1}, at::kByte, dev);
     }
     const int st = entry<decltype(&cts_kv_attention)>(a[0])(
         &p, &c, qr.p, qr.ld, static_cast<const int32_t*>(tp), static_cast<const int32_t*>(lp),

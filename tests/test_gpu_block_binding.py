@@ -28,3 +28,19 @@ def test_attention_of_all_queries_without_max_q(n_q, n_kv):
     assert not bool(torch.isnan(out).any())
     assert bool(((out.double() - want).abs() <= 2.0 ** -5 * (1 + want.abs())).all())
     assert np.array_equal(c["q_start"], np.concatenate(([0], np.cumsum(n_q))))
+
+
+def test_out_of_memory_keeps_its_type():
+    """A program that catches torch.OutOfMemoryError around the layer's calls catches it here."""
+    cache = cts.kv_cache(1, 16, 64, 256)
+    slots = torch.zeros(200000, dtype=torch.int64, device="cuda")        # 2 x 13 GB in fp32
+    say("kv_read past the allowed memory")
+    torch.cuda.empty_cache()
+    total = torch.cuda.get_device_properties(0).total_memory
+    torch.cuda.set_per_process_memory_fraction((torch.cuda.memory_reserved() + (1 << 30)) / total)
+    try:
+        with pytest.raises(torch.OutOfMemoryError):
+            cts.kv_read(cache, slots, dtype=torch.float32)
+    finally:
+        torch.cuda.set_per_process_memory_fraction(1.0)
+    assert cts.kv_read(cache, slots[:5])[0].shape == (5, 64, 256)
