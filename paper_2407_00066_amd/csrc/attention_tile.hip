@@ -218,9 +218,6 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prompt_kernel
     for (int i = tid; i < static_cast<int>(sizeof(sh.nan[0]) / 8); i += kThreads) (&sh.nan[which][0][0])[i] = 0;
   };
 
-#ifdef PRW
-  if ((blockIdx.x >> 8) & 1) __builtin_amdgcn_s_setprio(1);
-#endif
   clear(0);
   clear(1);
   clear(2);

@@ -7,8 +7,6 @@
 
 namespace cts {
 
-constexpr int kMxBlock = 32;      // elements that share a scale
-
 // n / d for n < 2^31 by a multiplication (a division by a number that only the
 // launch knows takes the GPU tens of instructions, a 64-bit one over a hundred).
 struct Divider {

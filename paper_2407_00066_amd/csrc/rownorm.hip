@@ -153,8 +153,13 @@ template <typename T, int THREADS, int V, bool NT> void norm_launch(const NormPa
   const int nv = (p.d + THREADS * V - 1) / (THREADS * V);
   const uint32_t grid = static_cast<uint32_t>((p.T + kRows - 1) / kRows);
   constexpr int kMost = 32 / V;
-  if (nv <= kMost / 4) block_norm_kernel<T, THREADS, V, kMost / 4, NT><<<grid, kBlock, 0, s>>>(p);
-  else if (nv <= kMost / 2) block_norm_kernel<T, THREADS, V, kMost / 2, NT><<<grid, kBlock, 0, s>>>(p);
+  if constexpr (THREADS == 64) {                    // (wider rows have more than 8 elements a thread)
+    if (nv <= kMost / 4) {
+      block_norm_kernel<T, THREADS, V, kMost / 4, NT><<<grid, kBlock, 0, s>>>(p);
+      return;
+    }
+  }
+  if (nv <= kMost / 2) block_norm_kernel<T, THREADS, V, kMost / 2, NT><<<grid, kBlock, 0, s>>>(p);
   else block_norm_kernel<T, THREADS, V, kMost, NT><<<grid, kBlock, 0, s>>>(p);
 }
 
@@ -279,10 +284,12 @@ template <typename T, int HEADS, bool NT> void rotary_launch(RotaryParams p, hip
 
 template <typename T> void rotary_typed(const RotaryParams& p, hipStream_t s) {
   // Angles shared by four heads where that leaves workgroups enough (6007 tokens of 40
-  // heads of 128 with 1, 2, 4 heads a thread: 47, 41, 37 us, before streaming stores).
+  // heads of 128 with 1, 2, 4 heads a thread: 47, 41, 37 us, before streaming stores);
+  // such outputs are of 32 MB and more.
   const int64_t n = static_cast<int64_t>(p.T) * (p.heads[0] + p.heads[1]) * (p.d / 16);
-  if (n < kRotThreads * 4 * 1024) rotary_launch<T, 1, false>(p, s);
-  else if (sizeof(T) * 16 * n < kStreamBytes) rotary_launch<T, 4, false>(p, s);
+  constexpr int64_t kShared = kRotThreads * 4 * 1024;
+  static_assert(kShared * 16 * sizeof(T) >= kStreamBytes);
+  if (n < kShared) rotary_launch<T, 1, false>(p, s);
   else rotary_launch<T, 4, true>(p, s);
 }
 
