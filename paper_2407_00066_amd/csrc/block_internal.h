@@ -19,6 +19,10 @@ struct Divider {
   __device__ __forceinline__ uint32_t operator()(uint32_t n) const { return (__umulhi(n, mul) + n) >> shift; }
 };
 
+// A launch has fewer than 2^32 threads along an axis: one with more runs what the low 32 bits
+// count, and reports success.
+constexpr int64_t max_groups(int threads) { return 0xffffffffll / threads; }
+
 // 16 bytes.  NT: stored past the caches.  Outputs of kStreamBytes and more are: ordinary
 // stores of that much hold up the loads beside them, and the next kernel loses
 // nothing (norm of T x 4096, bf16, ordinary / NT, alone and with a matrix product of n

@@ -184,9 +184,21 @@ template <typename T> bool vectors(const NormParams& p) {
   return (bits & 15) == 0;
 }
 
-template <typename T> void norm_typed(const NormParams& p, hipStream_t s) {
-  if (vectors<T>(p)) norm_rows<T, Elem<T>::N>(p, s);
-  else norm_rows<T, 1>(p, s);
+template <typename T> void norm_typed(NormParams p, hipStream_t s) {
+  constexpr int kMost = static_cast<int>(max_groups(1024));     // rows of a launch, whatever threads a row has
+  for (int left = p.T; left > 0; left -= kMost) {
+    p.T = std::min(left, kMost);
+    if (vectors<T>(p)) norm_rows<T, Elem<T>::N>(p, s);
+    else norm_rows<T, 1>(p, s);
+    if (left <= kMost) break;
+    p.x = static_cast<const T*>(p.x) + p.ldx * kMost;
+    p.n = static_cast<T*>(p.n) + p.ldn * kMost;
+    if (p.y) {
+      p.y = static_cast<const T*>(p.y) + p.ldy * kMost;
+      p.h = static_cast<T*>(p.h) + p.ldh * kMost;
+      if (p.gate) p.gate = static_cast<const T*>(p.gate) + p.ldg * kMost;
+    }
+  }
 }
 
 // ------------------------------------------------------------------- rotary
