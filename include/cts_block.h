@@ -9,8 +9,9 @@
  * Conventions are those of cts.h: array pointers are device memory owned by
  * the caller, structs and `sections` are host memory read during the call,
  * nothing is allocated or synchronised, calls only enqueue work on `stream`,
- * every argument error is found on the host before any HIP call, and T == 0 is
- * a no-op.  Arrays are 16-byte aligned (int32 arrays 4, int64 arrays 8) and
+ * every argument error is found on the host before any HIP call, T == 0 is
+ * a no-op, and a call of more work than a launch has threads for (137 GB of keys
+ * to write, 2^23 sequences x heads to attend to) is CTS_ERR_UNSUPPORTED.  Arrays are 16-byte aligned (int32 arrays 4, int64 arrays 8) and
  * rows of elements may lie further apart than they are long, as the slices of a
  * packed q/k/v output do: ld* are row strides in elements, multiples of 16
  * bytes, at least the row's length and at most 2^28.  dtype is CTS_BF16 or

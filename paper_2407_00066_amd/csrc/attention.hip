@@ -605,7 +605,8 @@ bool plan_attention(AttnParams* p, size_t* bytes) {
   int64_t span = p->max_kv;
   if (p->window) span = std::min<int64_t>(span, static_cast<int64_t>(p->window) + kRowTile + kUnit);
   const int64_t tiles = static_cast<int64_t>(p->B) * p->subs * p->c.heads;
-  if (tiles > 0x7fffffff || p->large_tiles * p->c.heads > 0x7fffffff) return false;
+  if (tiles > max_groups(64 * kWaves)) return false;
+  if (rows > kSmallRows && p->dtype == CTS_F32 && p->large_tiles * p->c.heads > max_groups(256)) return false;
   const int64_t most_steps = std::max<int64_t>(1, (span + kUnit - 1) / kUnit), steps = tiles * most_steps;
   if (steps > 0x50000000) return false;               // counted in 32 bits, rounded up to runs by less than a half
   // A tile's steps taken by one workgroup need no join, but last as long as the longest
@@ -626,7 +627,7 @@ bool plan_attention(AttnParams* p, size_t* bytes) {
     const int64_t all = static_cast<int64_t>(p->T) * p->group;
     p->prompt_tiles = (all + kPromptRows - 1) / kPromptRows + std::min<int64_t>(p->B, all / kSmallRows);
     const int64_t groups = std::max<int64_t>(1, p->prompt_tiles * p->c.heads);
-    if (groups > 0x7fffffff) return false;
+    if (groups > max_groups(kJoinThreads)) return false;             // (their kernel has as many threads)
     const int64_t most = std::max<int64_t>(1, span * p->c.d / 8192 / kPromptSteps);
     p->pieces = static_cast<int>(std::max<int64_t>(1, std::min(kPromptGroups / groups, most)));
     prompt_slots = std::min(kPromptGroups, groups * most);

@@ -15,7 +15,7 @@ using cts::Range;
 using cts::Rows;
 using cts::same;
 
-constexpr uint64_t kMaxGrid = 0x7fffffffull;
+constexpr uint64_t kMaxCount = 0x7fffffffull;     // of rows x heads, and of sequences x heads
 constexpr int64_t kMaxLd = int64_t{1} << 28;      // extents of 2^31 rows stay below 2^63 bytes
 
 uint64_t elt(int dtype) { return dtype == CTS_F32 ? 4 : 2; }
@@ -81,7 +81,7 @@ int check_kv(const cts_kv_cache* c, int32_t T, const void* k, int64_t ldk, const
   const Range sr{slots, 8ull * T};
   if (meets(extent(kr), r, 4) || meets(extent(vr), r, 4) || meets(sr, r, 4)) return CTS_ERR_INVALID_ARG;
   if (!write && (overlap(kr, vr) || overlap(extent(kr), sr) || overlap(extent(vr), sr))) return CTS_ERR_INVALID_ARG;
-  if (static_cast<uint64_t>(T) * width / 8 / 256 + 1 > kMaxGrid) return CTS_ERR_UNSUPPORTED;
+  if (!cts::kv_fits(*kc, T, write ? 8 : static_cast<int>(16 / elt(dtype)))) return CTS_ERR_UNSUPPORTED;
   return CTS_OK;
 }
 
@@ -104,7 +104,7 @@ int plan(const cts_attn_problem* p, const cts_kv_cache* c, cts::AttnParams* a, s
   a->max_kv = static_cast<int>(std::min<int64_t>(p->max_kv, room));
   a->scale_log2e = p->scale * 1.4426950408889634f;
   // (bounds that keep the plan's own arithmetic in 64 bits)
-  if (static_cast<uint64_t>(p->B) * c->n_heads > kMaxGrid || static_cast<uint64_t>(p->T) * p->n_q_heads > kMaxGrid)
+  if (static_cast<uint64_t>(p->B) * c->n_heads > kMaxCount || static_cast<uint64_t>(p->T) * p->n_q_heads > kMaxCount)
     return CTS_ERR_UNSUPPORTED;
   return cts::plan_attention(a, bytes) ? CTS_OK : CTS_ERR_UNSUPPORTED;
 }
@@ -239,7 +239,6 @@ int cts_rotary(int32_t T, int32_t n_q_heads, int32_t n_k_heads, int32_t head_dim
   if ((!same(qo, qi) && overlap(qo, qi)) || (!same(ko, ki) && overlap(ko, ki)) || overlap(qo, ki) || overlap(ko, qi) ||
       overlap(qo, ko) || meets(extent(qo), in, 3) || meets(extent(ko), in, 3))
     return CTS_ERR_INVALID_ARG;
-  if (static_cast<uint64_t>(T) * (wq + wk) / 8 / 256 + 1 > kMaxGrid) return CTS_ERR_UNSUPPORTED;
   a.T = T; a.heads[0] = n_q_heads; a.heads[1] = n_k_heads; a.d = head_dim; a.rot = rot_dim; a.n_pos = n_pos;
   a.axes = n_axes; a.interleaved = interleaved != 0;
   a.in[0] = q; a.ldi[0] = ldq; a.in[1] = k; a.ldi[1] = ldk;

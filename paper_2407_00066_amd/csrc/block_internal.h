@@ -43,6 +43,8 @@ struct KvCache {
   __host__ __device__ int64_t slots() const { return static_cast<int64_t>(n_pages) << page_shift; }
 };
 
+// Whether one launch takes T tokens, a thread `elements` of them at a time (8, or what 16 bytes hold).
+bool kv_fits(const KvCache& c, int T, int elements);
 hipError_t launch_kv_write(const KvCache& c, int T, const void* k, int64_t ldk, const void* v, int64_t ldv,
                            const int64_t* slots, int dtype, hipStream_t s);
 hipError_t launch_kv_read(const KvCache& c, int T, const int64_t* slots, void* k, int64_t ldk, void* v, int64_t ldv,
@@ -71,7 +73,7 @@ struct AttnParams {
 };
 
 // Chooses the plan and gives the workspace's bytes (not falling with any size);
-// false for a batch whose steps or workgroups 31 bits do not count.
+// false for a batch whose steps 31 bits do not count, or a launch has not the threads for.
 bool plan_attention(AttnParams* p, size_t* bytes);
 // Lays the workspace out for the plan.
 void place_attention(AttnParams* p, void* workspace);

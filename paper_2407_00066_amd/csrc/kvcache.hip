@@ -168,9 +168,12 @@ Work work_of(const KvCache& c, int T, int elements = 8) {
   const int64_t spread = (T + 1023) / 1024, full = (kThreads * kPieces + ne - 1) / ne;
   return {Divider(static_cast<uint32_t>(ne)), static_cast<int>(std::max<int64_t>(1, std::min(spread, full)))};
 }
-dim3 grid_of(const Work& w, int T) { return dim3(static_cast<uint32_t>((T + static_cast<int64_t>(w.tokens) - 1) / w.tokens), 2); }
+int64_t groups_of(const Work& w, int T) { return (T + static_cast<int64_t>(w.tokens) - 1) / w.tokens; }
+dim3 grid_of(const Work& w, int T) { return dim3(static_cast<uint32_t>(groups_of(w, T)), 2); }
 
 }  // namespace
+
+bool kv_fits(const KvCache& c, int T, int elements) { return groups_of(work_of(c, T, elements), T) <= max_groups(kThreads); }
 
 hipError_t launch_kv_write(const KvCache& c, int T, const void* k, int64_t ldk, const void* v, int64_t ldv,
                            const int64_t* slots, int dtype, hipStream_t s) {

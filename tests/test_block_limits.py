@@ -1,0 +1,38 @@
+"""Calls of more work than a launch has threads for are refused on the host (CPU;
+no call here reaches a kernel launch)."""
+import ctypes
+
+import pytest
+
+import paper_2407_00066_amd as cts
+from paper_2407_00066_amd import _binding as B
+
+from test_block_abi import UNSUPPORTED, _attend, _cache, _problem, _write
+
+GROUPS = 2 ** 24 - 1                  # workgroups of 256 threads that a launch can have
+
+
+@pytest.mark.parametrize("dtype,read,tokens", [(B.CTS_BF16, False, 32), (B.CTS_F32, False, 32), (B.CTS_BF16, True, 32),
+                                               (B.CTS_F32, True, 16)])
+def test_kv_calls_past_a_launch(dtype, read, tokens):
+    """tokens: of a workgroup, for two heads of 64."""
+    assert _write(T=GROUPS * tokens + 1, dtype=dtype, read=read) == UNSUPPORTED
+    assert _write(T=2 ** 31 - 1, dtype=dtype, read=read) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("kw", [
+    dict(T=2 ** 22, B=2 ** 22),                                         # 2^23 tiles of 512 threads
+    dict(T=2 ** 22, B=2 ** 21, max_q=2, n_q_heads=32),                  # two tiles a sequence
+    dict(T=2 ** 29 - 1, B=1, max_q=1000),                               # prompts of 128 rows a workgroup
+    dict(T=2 ** 27, B=1, max_q=1000, dtype=B.CTS_F32)])                 # 16 rows a workgroup
+def test_attention_past_a_launch(kw):
+    p, c = _problem(**kw), _cache()
+    assert cts.lib().cts_kv_attention_workspace_size(ctypes.byref(p), ctypes.byref(c)) == 0
+    assert _attend(p) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("kw", [dict(T=2 ** 22 - 1, B=2 ** 22 - 1), dict(T=2 ** 28, B=1, max_q=1000),
+                                dict(T=2 ** 26 - 64, B=1, max_q=1000, dtype=B.CTS_F32)])
+def test_attention_of_a_whole_launch_is_taken(kw):
+    p, c = _problem(**kw), _cache()
+    assert cts.lib().cts_kv_attention_workspace_size(ctypes.byref(p), ctypes.byref(c)) > 0
