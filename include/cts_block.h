@@ -95,7 +95,7 @@ typedef struct {
     int32_t max_kv;       /* kv_len, at most */
     int32_t window;       /* 0: none */
     int32_t dtype;        /* cts_dtype of q and out */
-    float scale;          /* > 0, commonly head_dim^-1/2 */
+    float scale;          /* > 0 and at most 2^127, commonly head_dim^-1/2 */
 } cts_attn_problem;
 
 /* Bytes of device workspace cts_kv_attention needs (0 for a problem it would

@@ -16,6 +16,7 @@ using cts::Rows;
 using cts::same;
 
 constexpr uint64_t kMaxCount = 0x7fffffffull;     // of rows x heads, and of sequences x heads
+constexpr float kLog2e = 1.4426950408889634f;
 constexpr int64_t kMaxLd = int64_t{1} << 28;      // extents of 2^31 rows stay below 2^63 bytes
 
 uint64_t elt(int dtype) { return dtype == CTS_F32 ? 4 : 2; }
@@ -90,7 +91,7 @@ int plan(const cts_attn_problem* p, const cts_kv_cache* c, cts::AttnParams* a, s
   const int e = check_cache_sizes(c);
   if (e != CTS_OK) return e;
   if (!p || p->T < 0 || p->B < 0 || p->n_q_heads < 1 || p->max_pages < 1 || p->max_q < 1 || p->max_kv < 0 ||
-      p->window < 0 || !(p->scale > 0.0f) || !std::isfinite(p->scale) || p->n_q_heads % c->n_heads != 0)
+      p->window < 0 || !(p->scale > 0.0f) || !std::isfinite(p->scale * kLog2e) || p->n_q_heads % c->n_heads != 0)
     return CTS_ERR_INVALID_ARG;
   if (!known(p->dtype) || p->n_q_heads > 65536 || p->max_q > (1 << 24) || p->max_kv > (1 << 30) || p->window > (1 << 30))
     return CTS_ERR_UNSUPPORTED;
@@ -102,7 +103,7 @@ int plan(const cts_attn_problem* p, const cts_kv_cache* c, cts::AttnParams* a, s
   a->max_pages = p->max_pages; a->max_q = p->max_q; a->window = p->window; a->dtype = p->dtype;
   const int64_t room = static_cast<int64_t>(p->max_pages) << shift;
   a->max_kv = static_cast<int>(std::min<int64_t>(p->max_kv, room));
-  a->scale_log2e = p->scale * 1.4426950408889634f;
+  a->scale_log2e = p->scale * kLog2e;
   // (bounds that keep the plan's own arithmetic in 64 bits)
   if (static_cast<uint64_t>(p->B) * c->n_heads > kMaxCount || static_cast<uint64_t>(p->T) * p->n_q_heads > kMaxCount)
     return CTS_ERR_UNSUPPORTED;

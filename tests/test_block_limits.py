@@ -7,7 +7,7 @@ import pytest
 import paper_2407_00066_amd as cts
 from paper_2407_00066_amd import _binding as B
 
-from test_block_abi import UNSUPPORTED, _attend, _cache, _problem, _write
+from test_block_abi import INVALID, UNSUPPORTED, _attend, _cache, _problem, _write
 
 GROUPS = 2 ** 24 - 1                  # workgroups of 256 threads that a launch can have
 
@@ -29,6 +29,13 @@ def test_attention_past_a_launch(kw):
     p, c = _problem(**kw), _cache()
     assert cts.lib().cts_kv_attention_workspace_size(ctypes.byref(p), ctypes.byref(c)) == 0
     assert _attend(p) == UNSUPPORTED
+
+
+def test_scale_past_the_exponent():
+    """The kernels' exponentials are of base 2: scale log2(e) has to be a float too."""
+    assert _attend(_problem(scale=3e38)) == INVALID
+    p, c = _problem(scale=2.0 ** 127), _cache()
+    assert cts.lib().cts_kv_attention_workspace_size(ctypes.byref(p), ctypes.byref(c)) > 0
 
 
 @pytest.mark.parametrize("kw", [dict(T=2 ** 22 - 1, B=2 ** 22 - 1), dict(T=2 ** 28, B=1, max_q=1000),
