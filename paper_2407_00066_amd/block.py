@@ -134,7 +134,10 @@ def kv_read(cache: KVCache, slots, dtype=torch.bfloat16, k_out=None, v_out=None)
 def kv_attention_workspace_size(q, cache: KVCache, B, max_q, max_kv, window=0) -> int:
     """Bytes of workspace kv_attention needs for queries like q of B sequences
     (0 for a call it would refuse)."""
-    p = AttnProblem(q.shape[0], B, q.shape[1], max(1, -(-max_kv // cache.page_size)), max_q, max_kv, window, _dt(q, "q"), 1.0)
+    sizes = (q.shape[0], B, q.shape[1], max(1, -(-max_kv // cache.page_size)), max_q, max_kv, window)
+    if not all(-2 ** 31 <= n < 2 ** 31 for n in sizes):
+        return 0                                        # (ctypes would take their low 32 bits)
+    p = AttnProblem(*sizes, _dt(q, "q"), 1.0)
     return int(lib().cts_kv_attention_workspace_size(ctypes.byref(p), ctypes.byref(cache._c)))
 
 

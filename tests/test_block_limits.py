@@ -3,6 +3,7 @@ no call here reaches a kernel launch)."""
 import ctypes
 
 import pytest
+import torch
 
 import paper_2407_00066_amd as cts
 from paper_2407_00066_amd import _binding as B
@@ -36,6 +37,13 @@ def test_scale_past_the_exponent():
     assert _attend(_problem(scale=3e38)) == INVALID
     p, c = _problem(scale=2.0 ** 127), _cache()
     assert cts.lib().cts_kv_attention_workspace_size(ctypes.byref(p), ctypes.byref(c)) > 0
+
+
+def test_workspace_size_of_sizes_past_32_bits():
+    cache, q = cts.kv_cache(2, 16, 2, 64, device="cpu"), torch.zeros(3, 4, 64)
+    assert cts.kv_attention_workspace_size(q, cache, 3, 1, 40) > 0
+    for kw in (dict(B=2 ** 32 + 3), dict(max_q=2 ** 32 + 1), dict(max_kv=2 ** 32 + 40), dict(window=2 ** 32 + 5)):
+        assert cts.kv_attention_workspace_size(q, cache, **{**dict(B=3, max_q=1, max_kv=40), **kw}) == 0, kw
 
 
 @pytest.mark.parametrize("kw", [dict(T=2 ** 22 - 1, B=2 ** 22 - 1), dict(T=2 ** 28, B=1, max_q=1000),
