@@ -5,7 +5,8 @@ them.
     python -m paper_2407_00066_amd.decoder [--requests 64] [--context 2000] [--layers 4]
 
 runs a prompt and then decode steps of a small stack on random weights and
-prints their times.
+prints their times: of the layers, and with the batch's preparation (its lists on
+the host, their copies, the sort of its tokens).
 
 The residual stream h and the last block's output y travel separately: the
 sum h + y is formed by the norm that reads it (block_norm).  Per block:
@@ -20,6 +21,7 @@ from __future__ import annotations
 
 import argparse
 import math
+import time
 
 import torch
 
@@ -123,6 +125,8 @@ def main(argv=None) -> None:
     ap.add_argument("--layers", type=int, default=4)
     ap.add_argument("--steps", type=int, default=8, help="decode steps")
     a = ap.parse_args(argv)
+    if min(a.requests, a.context, a.layers, a.steps) < 1:
+        ap.error("requests, context, layers and steps must be at least 1")
     d, heads, kv_heads, head_dim, d_ff, n, K, r, page = 4096, 32, 8, 128, 14336, 100, 4, 64, 16
     total = a.context + a.steps
     need = -(-total // page)
@@ -135,7 +139,11 @@ def main(argv=None) -> None:
 
     def step(requests, tokens, length):
         some = [adapters[i] for i in requests]
+        torch.cuda.synchronize()
+        t0 = time.perf_counter()
         batch = Batch(some, cluster_of, n, K, [tokens] * len(some), [length] * len(some), [tables[i] for i in requests], page)
+        torch.cuda.synchronize()
+        prepared = 1e3 * (time.perf_counter() - t0)
         h, y = torch.randn(batch.T, d, device="cuda").bfloat16(), None
         e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
         e0.record()
@@ -143,14 +151,20 @@ def main(argv=None) -> None:
             h, y = b.forward(h, y, batch)
         e1.record()
         e1.synchronize()
-        return e0.elapsed_time(e1)
+        ms = e0.elapsed_time(e1)
+        return ms, ms + prepared
+
+    def middle(times):
+        return sorted(times)[len(times) // 2]
 
     chunk = max(1, min(a.requests, 8192 // a.context))
     groups = [range(i, min(i + chunk, a.requests)) for i in range(0, a.requests, chunk)]
     ms = [step(g, a.context, a.context) for g in groups]
-    print("prompts: %d x %d tokens, %d layers: %.2f ms" % (a.requests, a.context, a.layers, sum(ms)))
+    print("prompts: %d x %d tokens, %d layers: %.2f ms, %.2f with the batches' preparation" %
+          (a.requests, a.context, a.layers, *map(sum, zip(*ms))))
     ms = [step(range(a.requests), 1, a.context + 1 + i) for i in range(a.steps)]
-    print("decode: %d requests, %d layers: %.3f ms a step" % (a.requests, a.layers, sorted(ms)[len(ms) // 2]))
+    print("decode: %d requests, %d layers: %.3f ms a step, %.3f with the batch's preparation" %
+          (a.requests, a.layers, *map(middle, zip(*ms))))
 
 
 if __name__ == "__main__":
