@@ -103,6 +103,18 @@ typedef struct {
  * B, max_q or max_kv grow, and a window never needs more than none. */
 size_t cts_kv_attention_workspace_size(const cts_attn_problem* p, const cts_kv_cache* c);
 
+/* How a call with these sizes takes its sequences, for tests and debugging; plan
+ * is a host array of 3 entries:
+ *   [0] tiles of 16 query rows (sequences of up to 64 rows of a key/value head, all in
+ *       f32): 0 a workgroup each, 1 the same by the sequences' lengths, 2 their
+ *       steps are dealt out in runs
+ *   [1] with 2: tiles (times heads, of those that have rows) up to which each is cut
+ *       into runs of its own; with more, runs go from tile to tile
+ *   [2] pieces that the tokens of the other sequences' tiles are split into (0:
+ *       max_q allows no such sequence, or f32)
+ * Errors as for the call's sizes. */
+int cts_kv_attention_plan(const cts_attn_problem* p, const cts_kv_cache* c, int32_t* plan);
+
 int cts_kv_attention(const cts_attn_problem* p, const cts_kv_cache* c, const void* q, int64_t ldq,
                      const int32_t* block_table, const int32_t* kv_len, const int32_t* q_start, void* out,
                      int64_t ldo, void* workspace, size_t workspace_bytes, void* stream);

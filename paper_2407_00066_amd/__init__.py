@@ -9,5 +9,5 @@ from ._binding import (CtsError, Problem, apply, apply_diag, apply_multi, apply_
                        bucketing_size, layer_plan, lib, make_problem, set_stage_events, sort_by_cluster, status_string,
                        validate_ids, workspace_bucketing, workspace_size, workspace_size_multi,
                        CTS_F32, CTS_BF16, NOALLOC_SCRATCH_BYTES)
-from .block import (KVCache, block_norm, kv_attention, kv_attention_workspace_size, kv_cache, kv_read, kv_write,  # noqa: F401
-                    rotary)
+from .block import (KVCache, block_norm, kv_attention, kv_attention_plan, kv_attention_workspace_size, kv_cache,  # noqa: F401
+                    kv_read, kv_write, rotary)

@@ -65,8 +65,8 @@ EXPORTED = ("cts_status_string", "cts_workspace_size", "cts_workspace_size_uncom
             "cts_jd_workspace_size", "cts_jd_cluster_workspace_size", "cts_lora_norms2", "cts_jd_full",
             "cts_jd_diag", "cts_jd_sigma", "cts_jd_cluster",
             # include/cts_block.h
-            "cts_kv_write", "cts_kv_read", "cts_kv_attention_workspace_size", "cts_kv_attention", "cts_block_norm",
-            "cts_rotary")
+            "cts_kv_write", "cts_kv_read", "cts_kv_attention_workspace_size", "cts_kv_attention_plan", "cts_kv_attention",
+            "cts_block_norm", "cts_rotary")
 N_STAGE_EVENTS = 6
 
 
@@ -177,6 +177,8 @@ def lib() -> ctypes.CDLL:
                 L.cts_kv_read.restype = ctypes.c_int
                 L.cts_kv_attention_workspace_size.argtypes = [ap, cp]
                 L.cts_kv_attention_workspace_size.restype = sz
+                L.cts_kv_attention_plan.argtypes = [ap, cp, ctypes.POINTER(i32)]
+                L.cts_kv_attention_plan.restype = ctypes.c_int
                 L.cts_kv_attention.argtypes = [ap, cp, vp, i64, vp, vp, vp, vp, i64, vp, sz, vp]
                 L.cts_kv_attention.restype = ctypes.c_int
                 L.cts_block_norm.argtypes = [i32, i32, i32, vp, i64, vp, i64, vp, vp, i64, fl, fl, vp, vp, i64, vp, i64, vp]

@@ -512,8 +512,8 @@ __global__ __launch_bounds__(64 * WAVES) void attn_tile_kernel(AttnParams p, int
   __shared__ __attribute__((aligned(16))) Shared<D, WAVES> sh;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int index = blockIdx.x / p.c.heads;
-  const int h = blockIdx.x - index * p.c.heads, tiles = p.B * p.subs * p.c.heads;
-  if (!large && tiles > 256 && tiles <= 512 && p.B <= 128 && p.max_kv >= 1024) {
+  const int h = blockIdx.x - index * p.c.heads;
+  if (!large && by_length(p)) {
     // Up to two workgroups for every compute unit: the longest sequences go first, and the
     // second workgroups take the others the other way round.  The waves look for the sequence
     // of that rank, each among its share of them.  32 + 8 heads of 128: 64 requests of 40 to
@@ -646,6 +646,12 @@ void place_attention(AttnParams* p, void* workspace) {
   p->part_ml = p->prompt_part + prompt * p->c.d;
   p->prompt_ml = p->part_ml + slots * 2;
   p->info = reinterpret_cast<int32_t*>(p->prompt_ml + prompt * 2);
+}
+
+void describe_attention(const AttnParams& p, int32_t* plan) {
+  plan[0] = !p.whole ? 2 : by_length(p) ? 1 : 0;
+  plan[1] = p.whole ? 0 : kFewTiles;
+  plan[2] = static_cast<int64_t>(p.max_q) * p.group > kSmallRows && p.dtype == CTS_BF16 ? p.pieces : 0;
 }
 
 hipError_t launch_attention(const AttnParams& p, hipStream_t s) {

@@ -115,6 +115,13 @@ struct Tile {                      // what a 16-row tile of a sequence covers
   int steps;                       // steps of kUnit tokens (one where nothing is seen); 0: no such rows
 };
 
+// Whether whole tiles take the sequences by their lengths: with up to two workgroups for every
+// compute unit, where lengths can differ enough for their order to matter.
+__host__ __device__ inline bool by_length(const AttnParams& p) {
+  const int tiles = p.B * p.subs * p.c.heads;
+  return tiles > 256 && tiles <= 512 && p.B <= 128 && p.max_kv >= 1024;
+}
+
 struct Queries { int q0, n; };     // a sequence's query rows
 __device__ __forceinline__ Queries queries_of(const AttnParams& p, int b) {
   if (!p.q_start) return {b, 1};

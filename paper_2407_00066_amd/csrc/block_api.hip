@@ -146,6 +146,16 @@ size_t cts_kv_attention_workspace_size(const cts_attn_problem* p, const cts_kv_c
   return plan(p, c, &a, &bytes) == CTS_OK ? bytes : 0;
 }
 
+int cts_kv_attention_plan(const cts_attn_problem* p, const cts_kv_cache* c, int32_t* how) {
+  cts::AttnParams a{};
+  size_t bytes = 0;
+  const int e = plan(p, c, &a, &bytes);
+  if (e != CTS_OK) return e;
+  if (!how) return CTS_ERR_INVALID_ARG;
+  cts::describe_attention(a, how);
+  return CTS_OK;
+}
+
 int cts_kv_attention(const cts_attn_problem* p, const cts_kv_cache* c, const void* q, int64_t ldq,
                      const int32_t* block_table, const int32_t* kv_len, const int32_t* q_start, void* out,
                      int64_t ldo, void* workspace, size_t workspace_bytes, void* stream) {

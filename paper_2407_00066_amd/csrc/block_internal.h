@@ -77,6 +77,8 @@ struct AttnParams {
 bool plan_attention(AttnParams* p, size_t* bytes);
 // Lays the workspace out for the plan.
 void place_attention(AttnParams* p, void* workspace);
+// The plan as cts_kv_attention_plan gives it.
+void describe_attention(const AttnParams& p, int32_t* plan);
 hipError_t launch_attention(const AttnParams& p, hipStream_t s);
 // The bf16 sequences with many query rows (attention_tile.hip).
 hipError_t launch_attention_prompts(const AttnParams& p, hipStream_t s);

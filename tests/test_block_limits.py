@@ -46,6 +46,23 @@ def test_workspace_size_of_sizes_past_32_bits():
         assert cts.kv_attention_workspace_size(q, cache, **{**dict(B=3, max_q=1, max_kv=40), **kw}) == 0, kw
 
 
+def test_attention_plan():
+    def plan(B_, max_q=1, max_kv=4000, kvh=8, heads=32, window=0, dtype=torch.bfloat16, cols=1 << 14):
+        cache = cts.kv_cache(1, 16, kvh, 128, device="cpu")
+        return cts.kv_attention_plan(torch.zeros(B_ * max_q, heads, 128, dtype=dtype), cache, torch.zeros(B_, cols), max_q,
+                                     max_kv, window)
+    assert plan(1, max_kv=700) == ("whole", 0, 0) and plan(1) == ("runs", 64, 0)
+    assert plan(64) == ("by length", 0, 0) and plan(65) == ("whole", 0, 0) and plan(64, max_kv=1000) == ("whole", 0, 0)
+    assert plan(64, max_kv=10000)[0] == "runs" and plan(64, max_kv=10000, cols=64)[0] == "by length"
+    assert plan(4, max_q=100, max_kv=300) == ("whole", 0, 1) and plan(1, max_q=100, max_kv=9000)[2] > 1
+    assert plan(4, max_q=100, max_kv=300, dtype=torch.float32)[2] == 0
+    assert plan(1, max_kv=9000, window=500)[0] == "whole"
+    p, c, out = _problem(), _cache(), (ctypes.c_int32 * 3)()
+    f = cts.lib().cts_kv_attention_plan
+    assert f(ctypes.byref(p), ctypes.byref(c), None) == INVALID and f(None, ctypes.byref(c), out) == INVALID
+    assert f(ctypes.byref(_problem(dtype=5)), ctypes.byref(c), out) == UNSUPPORTED
+
+
 @pytest.mark.parametrize("kw", [dict(T=2 ** 22 - 1, B=2 ** 22 - 1), dict(T=2 ** 28, B=1, max_q=1000),
                                 dict(T=2 ** 26 - 64, B=1, max_q=1000, dtype=B.CTS_F32)])
 def test_attention_of_a_whole_launch_is_taken(kw):
