@@ -39,6 +39,8 @@ class Batch:
                  device="cuda"):
         def i32(v):
             return torch.tensor(v, dtype=torch.int32, device=device)
+        if not counts or not all(0 <= n <= length for n, length in zip(counts, kv_len)):
+            raise ValueError("counts must be of one sequence or more, and of no more tokens than kv_len holds with them")
         ids, pos, slots, start = [], [], [], [0]
         for b, (n, length) in enumerate(zip(counts, kv_len)):
             ids += [adapter_of[b]] * n

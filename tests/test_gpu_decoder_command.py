@@ -2,6 +2,7 @@
 import re
 
 import pytest
+import torch
 
 from paper_2407_00066_amd import decoder
 
@@ -23,3 +24,11 @@ def test_times_with_and_without_the_preparation(capsys):
 def test_counts_of_zero_are_refused(name):
     with pytest.raises(SystemExit):
         decoder.main(["--" + name, "0"])
+
+
+@pytest.mark.parametrize("counts,kv_len", [([3], [2]), ([1, 5], [9, 4]), ([-1], [4]), ([], [])])
+def test_batch_refuses_tokens_before_the_first(counts, kv_len):
+    """A sequence's new tokens are among its cached ones: others would be written to pages of later ones."""
+    cluster_of = torch.zeros(2, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError, match="counts must be"):
+        decoder.Batch([0] * len(counts), cluster_of, 2, 1, counts, kv_len, [[0, 1]] * len(counts), 16)
