@@ -266,3 +266,25 @@ def test_nan_blocks_of_wide_heads(n_q, n_kv, max_kv, dtype):
     want = torch.zeros_like(out, dtype=torch.bool)
     want[see, 1, 160:192] = True
     assert torch.equal(torch.isnan(out), want)
+
+
+@pytest.mark.parametrize("n_q,dtype", [(70, "bf16"), (70, "f32"), (20, "bf16")])
+def test_pages_past_32_bits(n_q, dtype):
+    """Prompts whose pages' bytes lie past 2^32, beside one at the cache's start."""
+    pages, page, kvh, d = 2200, 1024, 32, 128                            # 4.6 GB of key codes
+    cache = cts.kv_cache(pages, page, kvh, d)
+    rng = np.random.default_rng(n_q)
+    slots = np.concatenate(((pages - 1) * page + np.arange(n_q), np.arange(n_q)))
+    k, v = (torch.from_numpy(rng.standard_normal((2 * n_q, kvh, d)).astype(np.float32)).cuda() for _ in range(2))
+    cts.kv_write(cache, k, v, torch.from_numpy(slots).cuda())
+    small = [torch.zeros_like(t[:2]) for t in (cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales)]
+    for t, s in zip((cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales), small):
+        s[0], s[1] = t[pages - 1], t[0]
+    q = torch.from_numpy(rng.standard_normal((2 * n_q, kvh, d)).astype(np.float32)).to(dtype=torch.float32 if dtype == "f32" else torch.bfloat16).cuda()
+    n_kv = torch.tensor([n_q, n_q], dtype=torch.int32, device="cuda")
+    start = torch.tensor([0, n_q, 2 * n_q], dtype=torch.int32, device="cuda")
+    say("kv_attention past 32 bits %s n=%d" % (dtype, n_q))
+    tables = [torch.tensor(t, dtype=torch.int32, device="cuda") for t in ([[pages - 1], [0]], [[0], [1]])]
+    got = cts.kv_attention(q, cache, tables[0], n_kv, q_start=start, max_q=n_q)
+    want = cts.kv_attention(q, cts.KVCache(*small), tables[1], n_kv, q_start=start, max_q=n_q)
+    assert torch.equal(got, want) and bool(want.any())
