@@ -81,8 +81,9 @@ int cts_kv_read(const cts_kv_cache* c, int32_t T, const int64_t* slots, void* k,
  * bf16 parts, which keep their 24 bits.
  * What is masked is never read into a result, whatever bytes stand there, NaN and
  * scales of 253 and 254 included.
- * max_q and max_kv bound the queries of a sequence and kv_len; tokens past
- * max_kv and queries past max_q are left out (out keeps what it held there).
+ * max_q and max_kv bound the queries of a sequence and kv_len.  A kv_len past
+ * max_kv, or past the table's max_pages, counts as that (P with it), one below 0
+ * as 0; queries past max_q, and rows of no sequence, are left out (out keeps what it held there).
  * They choose how the work is split and size the workspace.  A page number
  * outside [0, n_pages) reads as NaN; row and length arrays are clamped, so no
  * content makes a call read or write outside its arrays. */

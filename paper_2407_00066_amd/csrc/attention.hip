@@ -12,8 +12,8 @@
 //   query row.  Second: A row = element, k = tokens 4 g .. 4 g + 3 of two groups of 16.
 // Codes become bf16 in registers, two an instruction with their scale; nothing is
 // staged in shared memory.  Bound by the cache's bytes where there are many (64 requests of 4000
-// tokens: 57 us, 4.9 TB/s; four of 40000 to 131072: 78 us, 4.7 TB/s), by the chain of length,
-// page, codes and join where there are few (one of 709 tokens: 7.7 us).
+// tokens: 57 to 60 us, 4.7 to 4.9 TB/s; four of 40000 to 131072: 75 us, 4.9 TB/s), by the chain of
+// length, page, codes and join where there are few (one of 709 tokens: 7.4 us).
 #include <algorithm>
 
 #include "attention_common.h"
@@ -517,8 +517,8 @@ __global__ __launch_bounds__(64 * WAVES) void attn_tile_kernel(AttnParams p, int
     // Up to two workgroups for every compute unit: the longest sequences go first, and the
     // second workgroups take the others the other way round.  The waves look for the sequence
     // of that rank, each among its share of them.  32 + 8 heads of 128: 64 requests of 40 to
-    // 4000 tokens 41 / 33.5 us, of 1000 to 8000 79 / 66; 64 of 4000 each 57.2 / 58.6, of 300
-    // 9.8 / 10.8.  Where there are more workgroups they start as others end, and the order
+    // 4000 tokens 42 / 34.5 us, of 1000 to 8000 79 / 66; 64 of 4000 each 59.2 / 60.4 (in fp32
+    // 72.6 / 76), of 300 9.8 / 9.8.  Where there are more workgroups they start as others end, and the order
     // (longest first) matters less than what it takes: 128 of 4000 107.5 / 110, of 500 to 4000 68.9 / 67.6.
     __shared__ int found;
     const int b = index / p.subs, first = 256 / (p.subs * p.c.heads);

@@ -13,9 +13,10 @@
 //
 // Four waves of 32 rows, two such workgroups on a compute unit: one's softmax runs beside
 // the other's products.  Measured, prompts of 2048 (after 6144), 4096, 777 and 1301 tokens with
-// 32 + 8 heads of 128: 449 us, 885 TFLOP/s, where a library's large product
-// reaches 1400.  A step's 264 vector instructions and 32 matrix instructions of a wave
-// bound it together: the matrix pipe is busy for 40% of the time, and vector instructions
+// 32 + 8 heads of 128: 436 us, 910 TFLOP/s, where a library's large product reaches 1400 (461 on a
+// card where that reaches 1345); one of 4096 with heads of 64: 111 us, 618 TFLOP/s, 16 + 4 heads of
+// 256: 294 us, 467 (one wave a SIMD).  A step's 248 vector instructions and 32 matrix
+// instructions of a wave bound it together: the matrix pipe is busy for 40% of the time, and vector instructions
 // beside it run at two thirds of their rate.  Eight waves with one conversion for all
 // go in step at the barrier (525 us), also when the two halves take turns at vector work
 // and products (492 us); 64 rows a wave move their accumulators (722 us).
