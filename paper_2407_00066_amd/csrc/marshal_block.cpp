@@ -192,8 +192,8 @@ PyObject* cts_marshal_kv_attention(PyObject*, PyObject* const* a, Py_ssize_t n) 
     cts_attn_problem p{};
     p.T = int32(T); p.B = int32(B); p.n_q_heads = int32(heads); p.max_pages = int32(cols);
     p.dtype = dtype_code(dt);
-    // (all rows may be one sequence's; more than 2^24 queries of one are refused, and more rows than that are not)
-    p.max_q = a[9] != Py_None ? int32(a[9]) : a[8] == Py_None ? 1 : int32(std::clamp<int64_t>(T, 1, 1 << 24));
+    // (all rows may be one sequence's)
+    p.max_q = a[9] != Py_None ? int32(a[9]) : a[8] == Py_None ? 1 : int32(std::max<int64_t>(T, 1));
     p.max_kv = a[10] == Py_None ? int32(cols * c.page_size) : int32(a[10]);
     p.scale = static_cast<float>(number(a[11]));
     p.window = int32(a[12]);

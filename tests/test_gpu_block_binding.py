@@ -30,6 +30,22 @@ def test_attention_of_all_queries_without_max_q(n_q, n_kv):
     assert np.array_equal(c["q_start"], np.concatenate(([0], np.cumsum(n_q))))
 
 
+def test_more_rows_than_max_q_can_be():
+    """Without max_q, rows past the 2^24 that one sequence can have are refused, not left out; with it they are taken."""
+    T, B = 2 ** 24 + 2, 2
+    q = torch.zeros(T, 1, 64, dtype=torch.bfloat16, device="cuda")
+    cache = cts.kv_cache(2, 16, 1, 64)
+    table = torch.tensor([[0], [1]], dtype=torch.int32, device="cuda")
+    n = torch.tensor([3, 2], dtype=torch.int32, device="cuda")
+    start = torch.tensor([0, 1, 3], dtype=torch.int32, device="cuda")
+    say("kv_attention of %d rows" % T)
+    with pytest.raises(cts.CtsError):
+        cts.kv_attention(q, cache, table, n, q_start=start)
+    out = torch.full_like(q, 5.0)
+    cts.kv_attention(q, cache, table, n, q_start=start, max_q=B, out=out)
+    assert not out[:3].any() and bool((out[3:] == 5).all())
+
+
 def test_out_of_memory_keeps_its_type():
     """A program that catches torch.OutOfMemoryError around the layer's calls catches it here."""
     cache = cts.kv_cache(1, 16, 64, 256)
