@@ -3,8 +3,11 @@
  * layers (cts.h): a paged key/value cache held in 4 bits with its writes and
  * reads, the attention over it, the norms around a block with its residual,
  * and rotary positions.  A block then runs
- *   block_norm -> q/k/v layers -> rotary -> kv_write -> kv_attention -> o layer
- *   -> block_norm -> gate/up layers -> (activation) -> down layer -> block_norm
+ *   block_norm -> q/k/v layers -> kv_append (rotary and kv_write in one) ->
+ *   kv_attention -> o layer -> block_norm -> gate/up layers -> (activation)
+ *   -> down layer -> block_norm
+ * and a step that verifies trees of drafted tokens runs kv_tree_attention in the
+ * attention's place, and kv_keep once it is known which of them were accepted.
  *
  * Conventions are those of cts.h: array pointers are device memory owned by
  * the caller, structs and `sections` are host memory read during the call,
@@ -157,6 +160,53 @@ int cts_rotary(int32_t T, int32_t n_q_heads, int32_t n_k_heads, int32_t head_dim
                const void* q, int64_t ldq, const void* k, int64_t ldk, const float* cos, const float* sin,
                int32_t n_pos, const int32_t* positions, int32_t n_axes, const int32_t* sections,
                int32_t interleaved, void* q_out, int64_t ldqo, void* k_out, int64_t ldko, void* stream);
+
+/* New tokens' positions turned and their keys and values stored, in one launch:
+ * q_out = rotary(q), and kv_write of rotary(k) and v, equal by bits to
+ * cts_rotary followed by cts_kv_write (a turned key is rounded to dtype, then quantised).
+ * q [T][n_q_heads][head_dim] (n_q_heads may be 0, its pointers then NULL), k and v
+ * [T][n_heads][head_dim] with the cache's heads; slots as for cts_kv_write, the
+ * rest as for cts_rotary.  k_out (NULL: the turned keys go to the cache alone)
+ * receives the turned keys too, those of skipped slots among them.  q_out may be q and k_out k
+ * (same address and stride); otherwise outputs overlap nothing. */
+int cts_kv_append(const cts_kv_cache* c, int32_t T, int32_t n_q_heads, int32_t rot_dim, int32_t dtype, const void* q,
+                  int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, const int64_t* slots,
+                  const float* cos, const float* sin, int32_t n_pos, const int32_t* positions, int32_t n_axes,
+                  const int32_t* sections, int32_t interleaved, void* q_out, int64_t ldqo, void* k_out, int64_t ldko,
+                  void* stream);
+
+/* Attention of trees of drafted tokens.  Sizes, arrays and arithmetic are those of
+ * cts_kv_attention, but what a query sees is not its past: the n query rows of a sequence
+ * are drafts, whose keys and values are the sequence's last n cached tokens, in the rows'
+ * order, and row j sees
+ *   - the tokens before the drafts, t < kv_len - n; with a window, those with
+ *     t > P - window, P = positions[row] (int32 [T]; one before the first draft
+ *     counts as that draft's; positions are not read without a window);
+ *   - draft i if bit i % 32 of word i / 32 of its mask is set, i < n, whatever its
+ *     position (a row sees itself by its own bit; a window narrower than a
+ *     tree is the mask's to say).
+ * mask is uint32 [T][mask_words], mask_words >= (max_q + 31) / 32; bits past the
+ * sequence's drafts are ignored.  A row that sees nothing gives zeros; what no row
+ * of a sequence sees never reaches its results.  max_q is at most 512.  Queries past
+ * max_q are left out as rows, and as drafts that others see. */
+size_t cts_kv_tree_attention_workspace_size(const cts_attn_problem* p, const cts_kv_cache* c);
+
+int cts_kv_tree_attention(const cts_attn_problem* p, const cts_kv_cache* c, const void* q, int64_t ldq,
+                          const int32_t* block_table, const int32_t* kv_len, const int32_t* q_start, const uint32_t* mask,
+                          int64_t mask_words, const int32_t* positions, void* out, int64_t ldo, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+/* Keeps the accepted drafts of B sequences: the last n = q_start[b + 1] - q_start[b]
+ * (int32 [B + 1]) of a sequence's kv_len[b] cached tokens are drafts; draft
+ * path[b][i] (int32 [B][max_path], max_path at most 512) becomes its token kv_len[b] - n + i for
+ * every i < n_path[b] (int32; below 0 none, past max_path max_path).  Codes and scales
+ * move as they are, and all of a sequence's are read before any is written, whatever the
+ * path's order.  What lies outside a sequence's drafts or tokens, or on a page
+ * outside the cache, is neither read nor written; tokens past n_path[b] keep what they hold.
+ * kv_len itself is the caller's to set, to kv_len[b] - n + n_path[b].  Sequences whose tables share a page
+ * of drafts leave either's tokens there. */
+int cts_kv_keep(const cts_kv_cache* c, int32_t B, int32_t max_pages, const int32_t* block_table, const int32_t* kv_len,
+                const int32_t* q_start, int32_t max_path, const int32_t* path, const int32_t* n_path, void* stream);
 
 #ifdef __cplusplus
 }

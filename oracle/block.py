@@ -115,6 +115,66 @@ def attention(q, cache, table, kv_len, q_start, scale, window=0):
     return out, mag, soft
 
 
+def tree_attention(q, cache, table, kv_len, q_start, mask, scale, window=0, positions=None, max_q=None):
+    """attention's results for drafts: a sequence's rows are its last n cached tokens; row j sees the
+    tokens before them (with a window, t > positions[j] - window) and draft i if bit i of its mask
+    words is set.  Rows, and drafts, past max_q are left out (zeros here)."""
+    T, heads, d = q.shape
+    page, kvh = cache[0].shape[2], cache[0].shape[1]
+    out, mag, soft = np.zeros((T, heads, d)), np.zeros((T, heads, d)), np.zeros((T, heads, d))
+    for b, L in enumerate(kv_len):
+        L, q0, q1 = int(L), int(q_start[b]), int(q_start[b + 1])
+        n = q1 - q0
+        slots = [int(table[b][t // page]) * page + t % page for t in range(L)]
+        K, V = read(cache, slots)
+        count = n if max_q is None else min(n, max_q)
+        for j in range(count):
+            seen = []
+            for t in range(L):
+                if t < L - n:
+                    ok = not window or t > max(int(positions[q0 + j]), L - n) - window
+                else:
+                    i = t - (L - n)
+                    ok = i < count and bool(int(mask[q0 + j][i // 32]) >> (i % 32) & 1)
+                if ok:
+                    seen.append(t)
+            if not seen:
+                continue
+            for h in range(heads):
+                k, v = K[seen, h // (heads // kvh)], V[seen, h // (heads // kvh)]
+                s = scale * (k @ q[q0 + j, h])
+                e = (d + 8) * 2.0 ** -24 * scale * (np.abs(k) @ np.abs(q[q0 + j, h]))
+                w = np.exp(s - s.max())
+                w /= w.sum()
+                out[q0 + j, h] = w @ v
+                mag[q0 + j, h] = w @ np.abs(v)
+                soft[q0 + j, h] = mag[q0 + j, h] * (4 * e.max() + (len(seen) + d) * 2.0 ** -24)
+    return out, mag, soft
+
+
+def keep(cache, table, kv_len, q_start, path, n_path):
+    """The accepted drafts become the first ones, in place: all are read before any is written."""
+    page, n_pages = cache[0].shape[2], cache[0].shape[0]
+    for b, L in enumerate(kv_len):
+        n = int(q_start[b + 1]) - int(q_start[b])
+        past, moves = int(L) - n, []
+        for i in range(min(max(int(n_path[b]), 0), path.shape[1])):
+            f = int(path[b][i])
+            if not 0 <= f < n or past + f < 0 or not 0 <= past + i < L:
+                continue
+            src, dst = (int(table[b][(past + x) // page]) for x in (f, i))
+            if not (0 <= src < n_pages and 0 <= dst < n_pages):
+                continue
+            moves.append((dst, (past + i) % page, [_token(a, src, (past + f) % page, x >= 2).copy() for x, a in enumerate(cache)]))
+        for p, o, held in moves:
+            for x, a in enumerate(cache):
+                _token(a, p, o, x >= 2)[...] = held[x]
+
+
+def _token(a, p, o, value):
+    return a[p, :, o // 4, ..., o % 4, :] if value and a.ndim == 6 else a[p, :, o // 4, ..., o % 4] if value else a[p, :, o]
+
+
 # ---------------------------------------------------------------- norms, positions
 def block_norm(x, weight, y=None, post=None, gate=None, scale=1.0, eps=1e-6):
     """(h, n, |x| + |scale gate u|)."""

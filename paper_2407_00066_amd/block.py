@@ -1,6 +1,6 @@
 """What a decoder block needs around its multi-adapter layers
 (include/cts_block.h): the 4-bit key/value cache with its writes, reads and
-attention, the norms with the residual, and rotary positions.
+attention (of trees of drafted tokens too), the norms with the residual, and rotary positions.
 
 Argument marshalling only, like the layer's binding: every step runs in
 libcts.so's kernels, on torch's current stream.  Head arrays [T, heads,
@@ -213,6 +213,16 @@ def block_norm(x, weight, y=None, post_weight=None, gate=None, scale=1.0, eps=1e
     return (x if y is None else r[0]), r[1]
 
 
+def _check_angles(dev, T, cos, sin, positions, sections):
+    n_pos, half = cos.shape
+    _dev(cos, "cos", dev, F32, (n_pos, half))
+    _dev(sin, "sin", dev, F32, (n_pos, half))
+    axes = 1 if positions.dim() == 1 else positions.shape[0]
+    _dev(positions, "positions", dev, I32, (T,) if positions.dim() == 1 else (axes, T))
+    if sections is not None and len(sections) != axes:
+        raise ValueError("sections must hold a count for each of the %d axes" % axes)
+
+
 def rotary(q, k, cos, sin, positions, sections=None, interleaved=False, q_out=None, k_out=None):
     """(q', k'): q [T, n_q_heads, head_dim] and k [T, n_k_heads, head_dim]
     (either may be None) turned by the angles of cos, sin (fp32 [n_pos, rot_dim / 2])
@@ -237,13 +247,98 @@ def rotary(q, k, cos, sin, positions, sections=None, interleaved=False, q_out=No
             _rows(t, name, dev, tdt, shape)
             if o is not None:
                 _rows(o, name + "_out", dev, tdt, shape)
-        n_pos, half = cos.shape
-        _dev(cos, "cos", dev, F32, (n_pos, half))
-        _dev(sin, "sin", dev, F32, (n_pos, half))
-        axes = 1 if positions.dim() == 1 else positions.shape[0]
-        _dev(positions, "positions", dev, I32, (T,) if positions.dim() == 1 else (axes, T))
-        if sections is not None and len(sections) != axes:
-            raise ValueError("sections must hold a count for each of the %d axes" % axes)
+        _check_angles(dev, T, cos, sin, positions, sections)
         _refused(dev, "rotary")
     _check(r[2], "cts_rotary")
     return r[0], r[1]
+
+
+def kv_append(cache: KVCache, q, k, v, slots, cos, sin, positions, sections=None, interleaved=False, q_out=None, k_out=None):
+    """q' = rotary(q), and kv_write of rotary(k) and v [T, heads, head_dim], in one
+    launch and with the same bits; q (None: keys and values alone, and None is returned) is
+    [T, n_q_heads, head_dim].  k_out receives the turned keys too (None: the cache
+    alone does).  q_out, k_out may be q, k.  See rotary, kv_write and cts_kv_append."""
+    dev = cache.device
+    r = _native.kv_append(_entry("cts_kv_append"), _raw_stream(dev), dev, cache._at, q, k, v, slots, cos, sin, positions,
+                          sections, interleaved, q_out, k_out)
+    if r is None:
+        _dt(k, "k")
+        T, shape = k.shape[0], (k.shape[0], cache.n_heads, cache.head_dim)
+        if q is None and q_out is not None:
+            raise ValueError("q_out goes with q")
+        for t, name in ((k, "k"), (v, "v"), (k_out, "k_out")):
+            if t is not None or name != "k_out":
+                _rows(t, name, dev, k.dtype, shape)
+        for t, name in ((q, "q"), (q_out, "q_out")):
+            if t is not None:
+                _rows(t, name, dev, k.dtype, (T, q.shape[1], cache.head_dim))
+        _dev(slots, "slots", dev, I64, (T,))
+        _check_angles(dev, T, cos, sin, positions, sections)
+        _refused(dev, "kv_append")
+    _check(r[1], "cts_kv_append")
+    return r[0]
+
+
+def kv_tree_attention_workspace_size(q, cache: KVCache, B, max_q, max_kv, window=0) -> int:
+    """Bytes of workspace kv_tree_attention needs for queries like q of B
+    sequences (0 for a call it would refuse)."""
+    sizes = (q.shape[0], B, q.shape[1], max(1, -(-max_kv // cache.page_size)), max_q, max_kv, window)
+    if not all(-2 ** 31 <= n < 2 ** 31 for n in sizes):
+        return 0
+    p = AttnProblem(*sizes, _dt(q, "q"), 1.0)
+    return int(lib().cts_kv_tree_attention_workspace_size(ctypes.byref(p), ctypes.byref(cache._c)))
+
+
+def kv_tree_attention(q, cache: KVCache, block_table, kv_len, mask, q_start=None, max_q=None, max_kv=None, scale=None,
+                      window=0, positions=None, out=None, workspace=None):
+    """Attention of drafted tokens q [T, n_q_heads, head_dim]: each sequence's rows
+    are its last n cached tokens; a row sees the tokens before them (with a window, those
+    less than that before positions [T], int32) and the drafts whose bits its
+    mask [T, words] (int32, 32 drafts a word, the lowest bit first) has.  The rest
+    as for kv_attention; max_q (None: all rows of q, or as many as the mask has bits for)
+    is at most 512.  See cts_kv_tree_attention."""
+    dev = cache.device
+    r = _native.kv_tree_attention(_entry("cts_kv_tree_attention"), _entry("cts_kv_tree_attention_workspace_size"),
+                                  _raw_stream(dev), dev, cache._at, q, block_table, kv_len, mask, q_start, max_q, max_kv,
+                                  cache.head_dim ** -0.5 if scale is None else scale, window, positions, out, workspace)
+    if r is None:
+        _dt(q, "q")
+        shape = (q.shape[0], q.shape[1], cache.head_dim)
+        _rows(q, "q", dev, q.dtype, shape)
+        if out is not None:
+            _rows(out, "out", dev, q.dtype, shape)
+        B, cols = block_table.shape
+        _dev(block_table, "block_table", dev, I32, (B, cols))
+        _dev(kv_len, "kv_len", dev, I32, (B,))
+        if not isinstance(mask, torch.Tensor) or mask.dim() != 2:
+            raise ValueError("mask must be [T, words]")
+        _dev(mask, "mask", dev, I32, (q.shape[0], mask.shape[1]))
+        if q_start is not None:
+            _dev(q_start, "q_start", dev, I32, (B + 1,))
+        if positions is not None:
+            _dev(positions, "positions", dev, I32, (q.shape[0],))
+        if workspace is not None:
+            _dev(_binding._workspace(dev, 0, workspace), "workspace", dev, U8)
+        _refused(dev, "kv_tree_attention")
+    _check(r[1], "cts_kv_tree_attention")
+    return r[0]
+
+
+def kv_keep(cache: KVCache, block_table, kv_len, q_start, path, n_path) -> None:
+    """Keeps the accepted drafts: the last q_start[b + 1] - q_start[b] of sequence
+    b's kv_len[b] cached tokens are drafts, and draft path[b, i] becomes the i-th of
+    them for i < n_path[b] (path [B, max_path], n_path [B], int32).  The
+    sequence's length is the caller's to set.  See cts_kv_keep."""
+    dev = cache.device
+    st = _native.kv_keep(_entry("cts_kv_keep"), _raw_stream(dev), dev, cache._at, block_table, kv_len, q_start, path, n_path)
+    if st is None:
+        B, cols = block_table.shape
+        _dev(block_table, "block_table", dev, I32, (B, cols))
+        _dev(kv_len, "kv_len", dev, I32, (B,))
+        _dev(q_start, "q_start", dev, I32, (B + 1,))
+        if not isinstance(path, torch.Tensor) or path.dim() != 2:
+            raise ValueError("path must be [B, max_path]")
+        _dev(path, "path", dev, I32, (B, path.shape[1]))
+        _dev(n_path, "n_path", dev, I32, (B,))
+        _refused(dev, "kv_keep")
+    _check(st, "cts_kv_keep")

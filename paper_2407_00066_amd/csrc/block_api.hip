@@ -86,8 +86,8 @@ int check_kv(const cts_kv_cache* c, int32_t T, const void* k, int64_t ldk, const
   return CTS_OK;
 }
 
-// Sizes of an attention problem; fills the plan and the workspace's bytes.
-int plan(const cts_attn_problem* p, const cts_kv_cache* c, cts::AttnParams* a, size_t* bytes) {
+// Sizes of an attention problem, into a.
+int attention_sizes(const cts_attn_problem* p, const cts_kv_cache* c, cts::AttnParams* a) {
   const int e = check_cache_sizes(c);
   if (e != CTS_OK) return e;
   if (!p || p->T < 0 || p->B < 0 || p->n_q_heads < 1 || p->max_pages < 1 || p->max_q < 1 || p->max_kv < 0 ||
@@ -107,7 +107,66 @@ int plan(const cts_attn_problem* p, const cts_kv_cache* c, cts::AttnParams* a, s
   // (bounds that keep the plan's own arithmetic in 64 bits)
   if (static_cast<uint64_t>(p->B) * c->n_heads > kMaxCount || static_cast<uint64_t>(p->T) * p->n_q_heads > kMaxCount)
     return CTS_ERR_UNSUPPORTED;
+  return CTS_OK;
+}
+
+// The same with the plan and the workspace's bytes.
+int plan(const cts_attn_problem* p, const cts_kv_cache* c, cts::AttnParams* a, size_t* bytes) {
+  const int e = attention_sizes(p, c, a);
+  if (e != CTS_OK) return e;
   return cts::plan_attention(a, bytes) ? CTS_OK : CTS_ERR_UNSUPPORTED;
+}
+
+int plan(const cts_attn_problem* p, const cts_kv_cache* c, cts::TreeParams* a, size_t* bytes) {
+  const int e = attention_sizes(p, c, a);
+  if (e != CTS_OK) return e;
+  return p->max_q <= cts::kTreeMaxQ && cts::plan_tree(a, bytes) ? CTS_OK : CTS_ERR_UNSUPPORTED;
+}
+
+// The arrays of an attention call, into a: r has room for 8 ranges, which out may not meet
+// (the cache's, the table, the lengths, the rows and the workspace).
+int attention_arrays(const cts_attn_problem* p, const cts_kv_cache* c, const void* q, int64_t ldq,
+                     const int32_t* block_table, const int32_t* kv_len, const int32_t* q_start, void* out, int64_t ldo,
+                     void* workspace, size_t workspace_bytes, cts::AttnParams* a, Range* r) {
+  const int e = check_cache(c, &a->c, r);
+  if (e != CTS_OK) return e;
+  const int64_t width = static_cast<int64_t>(p->n_q_heads) * c->head_dim;
+  if (bad_rows(q, ldq, width, p->dtype) || bad_rows(out, ldo, width, p->dtype) || !block_table || !kv_len ||
+      misaligned(block_table, 4) || misaligned(kv_len, 4) || misaligned(q_start, 4) || !workspace ||
+      misaligned(workspace, 16))
+    return CTS_ERR_INVALID_ARG;
+  const Rows qr = rows(q, p->T, width, ldq, p->dtype), orr = rows(out, p->T, width, ldo, p->dtype);
+  r[4] = {block_table, 4ull * p->B * p->max_pages};
+  r[5] = {kv_len, 4ull * p->B};
+  r[6] = {q_start, q_start ? 4ull * (p->B + 1ull) : 0};
+  r[7] = {workspace, workspace_bytes};
+  if (meets(extent(orr), r, 8) || overlap(orr, qr) || meets(r[7], r, 7) || overlap(r[7], extent(qr)))
+    return CTS_ERR_INVALID_ARG;
+  a->q = q; a->ldq = ldq; a->out = out; a->ldo = ldo;
+  a->table = block_table; a->kv_len = kv_len; a->q_start = q_start;
+  return CTS_OK;
+}
+
+// Sizes and sections of a rotary call, into a; `heads` of its queries and keys.
+int rotary_sizes(int32_t T, int32_t n_q_heads, int32_t n_k_heads, int32_t head_dim, int32_t rot_dim, int32_t dtype,
+                 int32_t n_pos, int32_t n_axes, const int32_t* sections, int32_t interleaved, cts::RotaryParams* a) {
+  if (T < 0 || n_q_heads < 0 || n_k_heads < 0 || n_q_heads + static_cast<int64_t>(n_k_heads) < 1 || head_dim < 1 ||
+      rot_dim < 1 || rot_dim > head_dim || n_pos < 1 || n_axes < 1 || (n_axes > 1 && !sections))
+    return CTS_ERR_INVALID_ARG;
+  if (!known(dtype) || head_dim % 16 != 0 || rot_dim % 16 != 0 || head_dim > 4096 || n_axes > cts::kRotaryMaxAxes ||
+      n_q_heads > 65536 || n_k_heads > 65536)
+    return CTS_ERR_UNSUPPORTED;
+  int64_t sum = 0;
+  for (int i = 0; i < n_axes; ++i) {
+    const int32_t n = sections ? sections[i] : rot_dim / 2;
+    if (n < 0) return CTS_ERR_INVALID_ARG;
+    sum += n;
+    a->end[i] = static_cast<int>(std::min<int64_t>(sum, rot_dim / 2));
+  }
+  if (sum != rot_dim / 2) return CTS_ERR_INVALID_ARG;
+  a->T = T; a->heads[0] = n_q_heads; a->heads[1] = n_k_heads; a->d = head_dim; a->rot = rot_dim; a->n_pos = n_pos;
+  a->axes = n_axes; a->interleaved = interleaved != 0;
+  return CTS_OK;
 }
 
 }  // namespace
@@ -166,23 +225,9 @@ int cts_kv_attention(const cts_attn_problem* p, const cts_kv_cache* c, const voi
   if (!q_start && (p->max_q != 1 || p->T != p->B)) return CTS_ERR_INVALID_ARG;
   if (p->T == 0 || p->B == 0) return CTS_OK;
   Range r[8];
-  const int e2 = check_cache(c, &a.c, r);
+  const int e2 = attention_arrays(p, c, q, ldq, block_table, kv_len, q_start, out, ldo, workspace, workspace_bytes, &a, r);
   if (e2 != CTS_OK) return e2;
-  const int64_t width = static_cast<int64_t>(p->n_q_heads) * c->head_dim;
-  if (bad_rows(q, ldq, width, p->dtype) || bad_rows(out, ldo, width, p->dtype) || !block_table || !kv_len ||
-      misaligned(block_table, 4) || misaligned(kv_len, 4) || misaligned(q_start, 4) || !workspace ||
-      misaligned(workspace, 16))
-    return CTS_ERR_INVALID_ARG;
-  const Rows qr = rows(q, p->T, width, ldq, p->dtype), orr = rows(out, p->T, width, ldo, p->dtype);
-  r[4] = {block_table, 4ull * p->B * p->max_pages};
-  r[5] = {kv_len, 4ull * p->B};
-  r[6] = {q_start, q_start ? 4ull * (p->B + 1ull) : 0};
-  r[7] = {workspace, workspace_bytes};
-  if (meets(extent(orr), r, 8) || overlap(orr, qr) || meets(r[7], r, 7) || overlap(r[7], extent(qr)))
-    return CTS_ERR_INVALID_ARG;
   if (workspace_bytes < need) return CTS_ERR_WORKSPACE;
-  a.q = q; a.ldq = ldq; a.out = out; a.ldo = ldo;
-  a.table = block_table; a.kv_len = kv_len; a.q_start = q_start;
   cts::place_attention(&a, workspace);
   return status(cts::launch_attention(a, static_cast<hipStream_t>(stream)));
 }
@@ -221,21 +266,9 @@ int cts_rotary(int32_t T, int32_t n_q_heads, int32_t n_k_heads, int32_t head_dim
                const void* q, int64_t ldq, const void* k, int64_t ldk, const float* cos, const float* sin,
                int32_t n_pos, const int32_t* positions, int32_t n_axes, const int32_t* sections,
                int32_t interleaved, void* q_out, int64_t ldqo, void* k_out, int64_t ldko, void* stream) {
-  if (T < 0 || n_q_heads < 0 || n_k_heads < 0 || n_q_heads + static_cast<int64_t>(n_k_heads) < 1 || head_dim < 1 ||
-      rot_dim < 1 || rot_dim > head_dim || n_pos < 1 || n_axes < 1 || (n_axes > 1 && !sections))
-    return CTS_ERR_INVALID_ARG;
-  if (!known(dtype) || head_dim % 16 != 0 || rot_dim % 16 != 0 || head_dim > 4096 || n_axes > cts::kRotaryMaxAxes ||
-      n_q_heads > 65536 || n_k_heads > 65536)
-    return CTS_ERR_UNSUPPORTED;
   cts::RotaryParams a{};
-  int64_t sum = 0;
-  for (int i = 0; i < n_axes; ++i) {
-    const int32_t n = sections ? sections[i] : rot_dim / 2;
-    if (n < 0) return CTS_ERR_INVALID_ARG;
-    sum += n;
-    a.end[i] = static_cast<int>(std::min<int64_t>(sum, rot_dim / 2));
-  }
-  if (sum != rot_dim / 2) return CTS_ERR_INVALID_ARG;
+  const int e = rotary_sizes(T, n_q_heads, n_k_heads, head_dim, rot_dim, dtype, n_pos, n_axes, sections, interleaved, &a);
+  if (e != CTS_OK) return e;
   if (T == 0) return CTS_OK;
   const int64_t wq = static_cast<int64_t>(n_q_heads) * head_dim, wk = static_cast<int64_t>(n_k_heads) * head_dim;
   if ((wq && (bad_rows(q, ldq, wq, dtype) || bad_rows(q_out, ldqo, wq, dtype))) ||
@@ -250,12 +283,102 @@ int cts_rotary(int32_t T, int32_t n_q_heads, int32_t n_k_heads, int32_t head_dim
   if ((!same(qo, qi) && overlap(qo, qi)) || (!same(ko, ki) && overlap(ko, ki)) || overlap(qo, ki) || overlap(ko, qi) ||
       overlap(qo, ko) || meets(extent(qo), in, 3) || meets(extent(ko), in, 3))
     return CTS_ERR_INVALID_ARG;
-  a.T = T; a.heads[0] = n_q_heads; a.heads[1] = n_k_heads; a.d = head_dim; a.rot = rot_dim; a.n_pos = n_pos;
-  a.axes = n_axes; a.interleaved = interleaved != 0;
   a.in[0] = q; a.ldi[0] = ldq; a.in[1] = k; a.ldi[1] = ldk;
   a.out[0] = q_out; a.ldo[0] = ldqo; a.out[1] = k_out; a.ldo[1] = ldko;
   a.cos = cos; a.sin = sin; a.pos = positions;
   return status(cts::launch_rotary(a, dtype, static_cast<hipStream_t>(stream)));
+}
+
+size_t cts_kv_tree_attention_workspace_size(const cts_attn_problem* p, const cts_kv_cache* c) {
+  cts::TreeParams a{};
+  size_t bytes = 0;
+  return plan(p, c, &a, &bytes) == CTS_OK ? bytes : 0;
+}
+
+int cts_kv_tree_attention(const cts_attn_problem* p, const cts_kv_cache* c, const void* q, int64_t ldq,
+                          const int32_t* block_table, const int32_t* kv_len, const int32_t* q_start, const uint32_t* mask,
+                          int64_t mask_words, const int32_t* positions, void* out, int64_t ldo, void* workspace,
+                          size_t workspace_bytes, void* stream) {
+  cts::TreeParams a{};
+  size_t need = 0;
+  const int e = plan(p, c, &a, &need);
+  if (e != CTS_OK) return e;
+  if (!q_start && (p->max_q != 1 || p->T != p->B)) return CTS_ERR_INVALID_ARG;
+  if (mask_words < (p->max_q + 31) / 32 || mask_words > kMaxLd) return CTS_ERR_INVALID_ARG;
+  if (p->T == 0 || p->B == 0) return CTS_OK;
+  Range r[8];
+  const int e2 = attention_arrays(p, c, q, ldq, block_table, kv_len, q_start, out, ldo, workspace, workspace_bytes, &a, r);
+  if (e2 != CTS_OK) return e2;
+  if (!mask || misaligned(mask, 4) || (p->window && !positions) || misaligned(positions, 4)) return CTS_ERR_INVALID_ARG;
+  const Range more[2] = {{mask, 4ull * p->T * static_cast<uint64_t>(mask_words)},
+                         {positions, p->window ? 4ull * p->T : 0}};
+  const int64_t width = static_cast<int64_t>(p->n_q_heads) * c->head_dim;
+  if (meets(extent(rows(out, p->T, width, ldo, p->dtype)), more, 2) || meets(r[7], more, 2)) return CTS_ERR_INVALID_ARG;
+  if (workspace_bytes < need) return CTS_ERR_WORKSPACE;
+  a.mask = mask; a.mask_words = mask_words; a.positions = positions;
+  return status(cts::launch_tree(a, static_cast<hipStream_t>(stream)));
+}
+
+int cts_kv_keep(const cts_kv_cache* c, int32_t B, int32_t max_pages, const int32_t* block_table, const int32_t* kv_len,
+                const int32_t* q_start, int32_t max_path, const int32_t* path, const int32_t* n_path, void* stream) {
+  if (B < 0 || max_pages < 1 || max_path < 0) return CTS_ERR_INVALID_ARG;
+  const int e = check_cache_sizes(c);
+  if (e != CTS_OK) return e;
+  if (max_path > cts::kKeepMaxPath) return CTS_ERR_UNSUPPORTED;
+  if (B == 0 || max_path == 0) return CTS_OK;
+  cts::KvCache kc;
+  Range r[4];
+  const int e2 = check_cache(c, &kc, r);
+  if (e2 != CTS_OK) return e2;
+  for (const void* p : {block_table, kv_len, q_start, path, n_path})
+    if (!p || misaligned(p, 4)) return CTS_ERR_INVALID_ARG;
+  const Range in[5] = {{block_table, 4ull * B * max_pages}, {kv_len, 4ull * B}, {q_start, 4ull * (B + 1ull)},
+                       {path, 4ull * B * max_path}, {n_path, 4ull * B}};
+  for (const Range& a : in)
+    if (meets(a, r, 4)) return CTS_ERR_INVALID_ARG;
+  if (!cts::keep_fits(kc, B)) return CTS_ERR_UNSUPPORTED;
+  return status(cts::launch_kv_keep(kc, B, max_pages, block_table, kv_len, q_start, path, n_path, max_path,
+                                    static_cast<hipStream_t>(stream)));
+}
+
+int cts_kv_append(const cts_kv_cache* c, int32_t T, int32_t n_q_heads, int32_t rot_dim, int32_t dtype, const void* q,
+                  int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, const int64_t* slots,
+                  const float* cos, const float* sin, int32_t n_pos, const int32_t* positions, int32_t n_axes,
+                  const int32_t* sections, int32_t interleaved, void* q_out, int64_t ldqo, void* k_out, int64_t ldko,
+                  void* stream) {
+  const int e = check_cache_sizes(c);
+  if (e != CTS_OK) return e;
+  cts::RotaryParams a{};
+  const int e2 = rotary_sizes(T, n_q_heads, c->n_heads, c->head_dim, rot_dim, dtype, n_pos, n_axes, sections, interleaved, &a);
+  if (e2 != CTS_OK) return e2;
+  if (T == 0) return CTS_OK;
+  cts::KvCache kc;
+  const int e3 = check_kv(c, T, k, ldk, v, ldv, slots, dtype, true, &kc);
+  if (e3 != CTS_OK) return e3;
+  const int64_t wq = static_cast<int64_t>(n_q_heads) * c->head_dim, wk = static_cast<int64_t>(c->n_heads) * c->head_dim;
+  if ((wq && (bad_rows(q, ldq, wq, dtype) || bad_rows(q_out, ldqo, wq, dtype))) || (k_out && bad_rows(k_out, ldko, wk, dtype)) ||
+      !cos || !sin || !positions || misaligned(cos, 16) || misaligned(sin, 16) || misaligned(positions, 4))
+    return CTS_ERR_INVALID_ARG;
+  const Rows none{nullptr, 0, 0, 0};
+  const Rows qi = wq ? rows(q, T, wq, ldq, dtype) : none, qo = wq ? rows(q_out, T, wq, ldqo, dtype) : none;
+  const Rows ki = rows(k, T, wk, ldk, dtype), vi = rows(v, T, wk, ldv, dtype);
+  const Rows ko = k_out ? rows(k_out, T, wk, ldko, dtype) : none;
+  const size_t table = 2ull * rot_dim * n_pos;
+  Range r[4];
+  check_cache(c, &kc, r);
+  const Range in[4] = {{cos, table}, {sin, table}, {positions, 4ull * n_axes * T}, {slots, 8ull * T}};
+  if ((!same(qo, qi) && overlap(qo, qi)) || (!same(ko, ki) && overlap(ko, ki)) || overlap(qo, ki) || overlap(qo, vi) ||
+      overlap(ko, qi) || overlap(ko, vi) || overlap(qo, ko) || meets(extent(qi), r, 4))
+    return CTS_ERR_INVALID_ARG;
+  for (const Rows& o : {qo, ko})
+    if (meets(extent(o), in, 4) || meets(extent(o), r, 4)) return CTS_ERR_INVALID_ARG;
+  for (const Range& i : in)
+    if (meets(i, r, 4)) return CTS_ERR_INVALID_ARG;
+  a.in[0] = q; a.ldi[0] = ldq; a.in[1] = k; a.ldi[1] = ldk;
+  a.out[0] = q_out; a.ldo[0] = ldqo; a.out[1] = k_out; a.ldo[1] = ldko;
+  a.cos = cos; a.sin = sin; a.pos = positions;
+  if (!cts::append_fits(kc, a)) return CTS_ERR_UNSUPPORTED;
+  return status(cts::launch_kv_append(kc, a, v, ldv, slots, dtype, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

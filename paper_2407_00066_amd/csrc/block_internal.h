@@ -83,6 +83,17 @@ hipError_t launch_attention(const AttnParams& p, hipStream_t s);
 // The bf16 sequences with many query rows (attention_tile.hip).
 hipError_t launch_attention_prompts(const AttnParams& p, hipStream_t s);
 
+// Attention of drafted tokens (attention_tree.hip): max_q is at most kTreeMaxQ; subs tiles of
+// tile_rows rows (query x head of a key/value head's group) of a sequence.
+constexpr int kTreeMaxQ = 512;
+struct TreeParams : AttnParams {
+  const uint32_t* mask; int64_t mask_words;     // [T][mask_words]
+  const int32_t* positions;                     // of the rows, with a window
+  int tile_rows;
+};
+bool plan_tree(TreeParams* p, size_t* bytes);
+hipError_t launch_tree(const TreeParams& p, hipStream_t s);
+
 struct NormParams {
   int T, d;
   const void *x, *y, *post, *gate, *weight;
@@ -104,5 +115,16 @@ struct RotaryParams {
   int end[kRotaryMaxAxes];          // pairs of the axes up to this one
 };
 hipError_t launch_rotary(const RotaryParams& p, int dtype, hipStream_t s);
+
+// r: the queries [0] (none: 0 heads) and the keys [1], whose turned rows go to out[1] too, or nowhere.
+// Whether one launch takes them.
+bool append_fits(const KvCache& c, const RotaryParams& r);
+hipError_t launch_kv_append(const KvCache& c, const RotaryParams& r, const void* v, int64_t ldv, const int64_t* slots,
+                            int dtype, hipStream_t s);
+
+constexpr int kKeepMaxPath = 512;   // accepted drafts of a sequence
+bool keep_fits(const KvCache& c, int B);
+hipError_t launch_kv_keep(const KvCache& c, int B, int max_pages, const int32_t* table, const int32_t* kv_len,
+                          const int32_t* q_start, const int32_t* path, const int32_t* n_path, int max_path, hipStream_t s);
 
 }  // namespace cts

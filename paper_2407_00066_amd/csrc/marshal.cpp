@@ -18,6 +18,9 @@ PyObject* cts_marshal_kv_read(PyObject*, PyObject* const*, Py_ssize_t);
 PyObject* cts_marshal_kv_attention(PyObject*, PyObject* const*, Py_ssize_t);
 PyObject* cts_marshal_block_norm(PyObject*, PyObject* const*, Py_ssize_t);
 PyObject* cts_marshal_rotary(PyObject*, PyObject* const*, Py_ssize_t);
+PyObject* cts_marshal_kv_append(PyObject*, PyObject* const*, Py_ssize_t);
+PyObject* cts_marshal_kv_tree_attention(PyObject*, PyObject* const*, Py_ssize_t);
+PyObject* cts_marshal_kv_keep(PyObject*, PyObject* const*, Py_ssize_t);
 
 namespace {
 
@@ -63,6 +66,9 @@ PyMethodDef methods[] = {
     {"kv_attention", method(cts_marshal_kv_attention), METH_FASTCALL, "cts_kv_attention, its tensors checked"},
     {"block_norm", method(cts_marshal_block_norm), METH_FASTCALL, "cts_block_norm, its tensors checked"},
     {"rotary", method(cts_marshal_rotary), METH_FASTCALL, "cts_rotary, its tensors checked"},
+    {"kv_append", method(cts_marshal_kv_append), METH_FASTCALL, "cts_kv_append, its tensors checked"},
+    {"kv_tree_attention", method(cts_marshal_kv_tree_attention), METH_FASTCALL, "cts_kv_tree_attention, its tensors checked"},
+    {"kv_keep", method(cts_marshal_kv_keep), METH_FASTCALL, "cts_kv_keep, its tensors checked"},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

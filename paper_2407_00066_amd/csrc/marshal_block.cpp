@@ -116,6 +116,23 @@ const cts_kv_cache& cache_of(PyObject* o) {
   return *reinterpret_cast<const cts_kv_cache*>(static_cast<uintptr_t>(integer(o)));
 }
 
+// The sections of a rotary call (host numbers, one for each axis), into sec; null for None.
+const int32_t* sections_of(PyObject* given, int64_t axes, int32_t* sec) {
+  if (given == Py_None) return nullptr;
+  PyObject* list = PySequence_Fast(given, "sections");
+  need(list != nullptr);
+  const bool fits = PySequence_Fast_GET_SIZE(list) == axes && axes <= 16;
+  bool ok = fits;
+  for (int64_t i = 0; ok && i < axes; ++i) {
+    const long long v = PyLong_AsLongLong(PySequence_Fast_GET_ITEM(list, i));
+    ok = !(v == -1 && PyErr_Occurred()) && v >= INT32_MIN && v <= INT32_MAX;
+    sec[i] = static_cast<int32_t>(v);
+  }
+  Py_DECREF(list);
+  need(ok);
+  return sec;
+}
+
 PyObject* wrap(const at::Tensor& t) { return THPVariable_Wrap(t); }
 
 // Runs f; None for a refusal, and for tensors whose sizes or storage cannot be had (they
@@ -281,19 +298,7 @@ PyObject* cts_marshal_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
       out[i] = rows(*o[i], dev, dt, shape);
     }
     int32_t sec[16];
-    if (a[8] != Py_None) {
-      PyObject* list = PySequence_Fast(a[8], "sections");
-      need(list != nullptr);
-      const bool fits = PySequence_Fast_GET_SIZE(list) == axes && axes <= 16;
-      bool ok = fits;
-      for (int64_t i = 0; ok && i < axes; ++i) {
-        const long long v = PyLong_AsLongLong(PySequence_Fast_GET_ITEM(list, i));
-        ok = !(v == -1 && PyErr_Occurred()) && v >= INT32_MIN && v <= INT32_MAX;
-        sec[i] = static_cast<int32_t>(v);
-      }
-      Py_DECREF(list);
-      need(ok);
-    }
+    const int32_t* const sections = sections_of(a[8], axes, sec);
     const void* cp = dense(cos, dev, at::kFloat, {n_pos, half});
     const void* sp = dense(tensor(a[6]), dev, at::kFloat, {n_pos, half});
     const void* pp = pos.dim() == 1 ? dense(pos, dev, at::kInt, {T}) : dense(pos, dev, at::kInt, {axes, T});
@@ -302,12 +307,120 @@ PyObject* cts_marshal_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int st = entry<decltype(&cts_rotary)>(a[0])(
         int32(T), int32(heads[0]), int32(heads[1]), int32(d), int32(2 * half), code, in[0].p, in[0].ld, in[1].p, in[1].ld,
         static_cast<const float*>(cp), static_cast<const float*>(sp), int32(n_pos), static_cast<const int32_t*>(pp),
-        int32(axes), a[8] == Py_None ? nullptr : sec, inter, out[0].p, out[0].ld, out[1].p, out[1].ld, stream(a[1]));
+        int32(axes), sections, inter, out[0].p, out[0].ld, out[1].p, out[1].ld, stream(a[1]));
     PyObject* r[2];
     for (int i = 0; i < 2; ++i) {
       if (o[i]) r[i] = wrap(*o[i]);
       else { Py_INCREF(Py_None); r[i] = Py_None; }
     }
     return Py_BuildValue("(NNi)", r[0], r[1], st);
+  });
+}
+
+// kv_append(entry, stream, device, cache, q, k, v, slots, cos, sin, positions, sections, interleaved, q_out, k_out)
+//   -> (q', status)
+PyObject* cts_marshal_kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 15, [&]() -> PyObject* {
+    const c10::Device dev = device_of(a[2]);
+    const cts_kv_cache& c = cache_of(a[3]);
+    const at::Tensor &k = tensor(a[5]), &v = tensor(a[6]), &slots = tensor(a[7]), &cos = tensor(a[8]), &pos = tensor(a[10]);
+    const c10::ScalarType dt = k.scalar_type();
+    const int code = dtype_code(dt);
+    need(k.dim() == 3 && cos.dim() == 2 && (pos.dim() == 1 || pos.dim() == 2));
+    const int64_t T = k.size(0), n_pos = cos.size(0), half = cos.size(1), axes = pos.dim() == 1 ? 1 : pos.size(0);
+    const int64_t shape[3] = {T, c.n_heads, c.head_dim};
+    const Rows kr = rows(k, dev, dt, shape), vr = rows(v, dev, dt, shape);
+    const void* s = dense(slots, dev, at::kLong, {T});
+    Rows qr{}, qo{}, ko{};
+    int64_t heads = 0;
+    std::optional<at::Tensor> out;
+    if (a[4] != Py_None) {
+      const at::Tensor& q = tensor(a[4]);
+      need(q.dim() == 3);
+      heads = q.size(1);
+      const int64_t q_shape[3] = {T, heads, c.head_dim};
+      qr = rows(q, dev, dt, q_shape);
+      out = fresh(a[13], q_shape, dt, dev);
+      qo = rows(*out, dev, dt, q_shape);
+    } else {
+      need(a[13] == Py_None);
+    }
+    if (a[14] != Py_None) ko = rows(tensor(a[14]), dev, dt, shape);
+    const void* cp = dense(cos, dev, at::kFloat, {n_pos, half});
+    const void* sp = dense(tensor(a[9]), dev, at::kFloat, {n_pos, half});
+    const void* pp = pos.dim() == 1 ? dense(pos, dev, at::kInt, {T}) : dense(pos, dev, at::kInt, {axes, T});
+    int32_t sec[16];
+    const int32_t* const sections = sections_of(a[11], axes, sec);
+    const int inter = PyObject_IsTrue(a[12]);
+    need(inter >= 0);
+    const int st = entry<decltype(&cts_kv_append)>(a[0])(
+        &c, int32(T), int32(heads), int32(2 * half), code, qr.p, qr.ld, kr.p, kr.ld, vr.p, vr.ld,
+        static_cast<const int64_t*>(s), static_cast<const float*>(cp), static_cast<const float*>(sp), int32(n_pos),
+        static_cast<const int32_t*>(pp), int32(axes), sections, inter, qo.p, qo.ld, ko.p, ko.ld, stream(a[1]));
+    if (out) return Py_BuildValue("(Ni)", wrap(*out), st);
+    return Py_BuildValue("(Oi)", Py_None, st);
+  });
+}
+
+// kv_tree_attention(entry, size entry, stream, device, cache, q, block_table, kv_len, mask, q_start, max_q, max_kv, scale,
+//                   window, positions, out, workspace) -> (out, status)
+PyObject* cts_marshal_kv_tree_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 17, [&]() -> PyObject* {
+    const c10::Device dev = device_of(a[3]);
+    const cts_kv_cache& c = cache_of(a[4]);
+    const at::Tensor &q = tensor(a[5]), &table = tensor(a[6]), &len = tensor(a[7]), &mask = tensor(a[8]);
+    const c10::ScalarType dt = q.scalar_type();
+    need(q.dim() == 3 && table.dim() == 2 && mask.dim() == 2);
+    const int64_t T = q.size(0), heads = q.size(1), B = table.size(0), cols = table.size(1), words = mask.size(1);
+    const int64_t shape[3] = {T, heads, c.head_dim};
+    const Rows qr = rows(q, dev, dt, shape);
+    cts_attn_problem p{};
+    p.T = int32(T); p.B = int32(B); p.n_q_heads = int32(heads); p.max_pages = int32(cols);
+    p.dtype = dtype_code(dt);
+    // (no sequence has more drafts than rows, or than the mask has bits for)
+    p.max_q = a[10] != Py_None ? int32(a[10]) : a[9] == Py_None ? 1 : int32(std::max<int64_t>(std::min(T, 32 * words), 1));
+    p.max_kv = a[11] == Py_None ? int32(cols * c.page_size) : int32(a[11]);
+    p.scale = static_cast<float>(number(a[12]));
+    p.window = int32(a[13]);
+    const void* tp = dense(table, dev, at::kInt, {B, cols});
+    const void* lp = dense(len, dev, at::kInt, {B});
+    const void* mp = dense(mask, dev, at::kInt, {T, words});
+    const void* sp = a[9] == Py_None ? nullptr : dense(tensor(a[9]), dev, at::kInt, {B + 1});
+    const void* pp = a[14] == Py_None ? nullptr : dense(tensor(a[14]), dev, at::kInt, {T});
+    const at::Tensor out = fresh(a[15], shape, dt, dev);
+    const Rows orr = rows(out, dev, dt, shape);
+    at::Tensor ws;
+    if (a[16] != Py_None) {
+      ws = tensor(a[16]);
+      need(ws.device() == dev && ws.scalar_type() == at::kByte && ws.is_contiguous());
+    } else {
+      const int64_t bytes = entry<decltype(&cts_kv_tree_attention_workspace_size)>(a[1])(&p, &c);
+      ws = allocate({bytes > 0 ? bytes : 1}, at::kByte, dev);
+    }
+    const int st = entry<decltype(&cts_kv_tree_attention)>(a[0])(
+        &p, &c, qr.p, qr.ld, static_cast<const int32_t*>(tp), static_cast<const int32_t*>(lp),
+        static_cast<const int32_t*>(sp), static_cast<const uint32_t*>(mp), words, static_cast<const int32_t*>(pp), orr.p,
+        orr.ld, data(ws), static_cast<size_t>(ws.numel()), stream(a[2]));
+    return Py_BuildValue("(Ni)", wrap(out), st);
+  });
+}
+
+// kv_keep(entry, stream, device, cache, block_table, kv_len, q_start, path, n_path) -> status
+PyObject* cts_marshal_kv_keep(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 9, [&]() -> PyObject* {
+    const c10::Device dev = device_of(a[2]);
+    const cts_kv_cache& c = cache_of(a[3]);
+    const at::Tensor &table = tensor(a[4]), &path = tensor(a[7]);
+    need(table.dim() == 2 && path.dim() == 2);
+    const int64_t B = table.size(0), cols = table.size(1), most = path.size(1);
+    const void* tp = dense(table, dev, at::kInt, {B, cols});
+    const void* lp = dense(tensor(a[5]), dev, at::kInt, {B});
+    const void* sp = dense(tensor(a[6]), dev, at::kInt, {B + 1});
+    const void* pp = dense(path, dev, at::kInt, {B, most});
+    const void* np = dense(tensor(a[8]), dev, at::kInt, {B});
+    return PyLong_FromLong(entry<decltype(&cts_kv_keep)>(a[0])(
+        &c, int32(B), int32(cols), static_cast<const int32_t*>(tp), static_cast<const int32_t*>(lp),
+        static_cast<const int32_t*>(sp), int32(most), static_cast<const int32_t*>(pp), static_cast<const int32_t*>(np),
+        stream(a[1])));
   });
 }

@@ -5,51 +5,10 @@
 #include <algorithm>
 
 #include "block_internal.h"
+#include "rows.h"
 
 namespace cts {
 namespace {
-
-template <typename T> struct Elem;
-template <> struct Elem<float> {
-  static constexpr int N = 4;                       // elements of 16 bytes
-  __device__ static __forceinline__ float get(const float* p) { return *p; }
-  __device__ static __forceinline__ void put(float* p, float v) { *p = v; }
-  __device__ static __forceinline__ void get16(const float* p, float* f) {
-    const float4 v = *reinterpret_cast<const float4*>(p);
-    f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w;
-  }
-  template <bool NT> __device__ static __forceinline__ void put16(float* p, const float* f) {
-    store16<NT>(p, __float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
-  }
-};
-template <> struct Elem<bf16_t> {
-  static constexpr int N = 8;
-  __device__ static __forceinline__ float get(const bf16_t* p) { return bf16_to_f32(p->bits); }
-  __device__ static __forceinline__ void put(bf16_t* p, float v) { p->bits = f32_to_bf16(v); }
-  __device__ static __forceinline__ void get16(const bf16_t* p, float* f) {
-    const uint4 v = *reinterpret_cast<const uint4*>(p);
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      f[2 * i] = __uint_as_float(w[i] << 16);
-      f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-  }
-  template <bool NT> __device__ static __forceinline__ void put16(bf16_t* p, const float* f) {
-    store16<NT>(p, f32_to_bf16_pair(f[0], f[1]), f32_to_bf16_pair(f[2], f[3]), f32_to_bf16_pair(f[4], f[5]),
-                f32_to_bf16_pair(f[6], f[7]));
-  }
-};
-
-// V consecutive elements: one 16-byte access, or one element
-template <typename T, int V> __device__ __forceinline__ void get(const T* p, float* f) {
-  if constexpr (V == 1) f[0] = Elem<T>::get(p);
-  else Elem<T>::get16(p, f);
-}
-template <typename T, int V, bool NT> __device__ __forceinline__ void put(T* p, const float* f) {
-  if constexpr (V == 1) Elem<T>::put(p, f[0]);
-  else Elem<T>::template put16<NT>(p, f);
-}
 
 // V elements at `at`, zeros past the row's end (d is a multiple of V): the address is
 // clamped instead of the load skipped, so that all of a row's loads go out together.
@@ -204,88 +163,14 @@ template <typename T> void norm_typed(NormParams p, hipStream_t s) {
 // ------------------------------------------------------------------- rotary
 constexpr int kRotThreads = 256;
 
-// A thread turns 8 pairs of a head (with halves, 8 elements of each half; interleaved, 16
-// consecutive ones) or copies 8 elements past rot, for HEADS heads that share the
-// pairs' angles: their cosines and sines are loaded once for all of them.
 template <typename T, int HEADS, bool NT>
 __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotaryParams p, int64_t t0, int n) {
-  constexpr int N = Elem<T>::N;
   const int i = blockIdx.x * kRotThreads + threadIdx.x;
-  if (i >= n) return;
-  const int64_t t = t0 + p.per_token(i);
-  const int in_token = i - p.per_token(i) * p.per_token.d;
-  const int group = p.per_head(in_token), piece = in_token - group * p.per_head.d;
-  const int heads = p.heads[0] + p.heads[1], groups = (heads + HEADS - 1) / HEADS;
-  const int pieces = p.rot / 16, half = p.rot / 2;
-  const bool turns = piece < pieces;
-  const int j0 = piece * 8;                       // the first pair
-  const int at0 = !turns ? p.rot + (piece - pieces) * 8 : p.interleaved ? 2 * j0 : j0;
-  const int at1 = p.interleaved ? 2 * j0 + 8 : j0 + half;
-  float a[HEADS][16];
-  T* o[HEADS];
-#pragma unroll
-  for (int k = 0; k < HEADS; ++k) {
-    const int all = group + k * groups;
-    o[k] = nullptr;
-    if (all >= heads) continue;
-    const int which = all >= p.heads[0], head = which ? all - p.heads[0] : all;
-    const T* x = static_cast<const T*>(p.in[which]) + t * p.ldi[which] + static_cast<int64_t>(head) * p.d;
-    o[k] = static_cast<T*>(p.out[which]) + t * p.ldo[which] + static_cast<int64_t>(head) * p.d;
-#pragma unroll
-    for (int e = 0; e < 8; e += N) get<T, N>(x + at0 + e, a[k] + e);
-    if (turns)
-#pragma unroll
-      for (int e = 0; e < 8; e += N) get<T, N>(x + at1 + e, a[k] + 8 + e);
-  }
-  if (turns) {
-    float c[8], s[8];
-    int axis = 0;
-    while (axis + 1 < p.axes && j0 >= p.end[axis]) ++axis;
-    auto row = [&](int ax) {
-      return static_cast<int64_t>(min(max(p.pos[static_cast<int64_t>(ax) * p.T + t], 0), p.n_pos - 1)) * half + j0;
-    };
-    if (j0 + 8 <= p.end[axis]) {                  // one axis: 32 bytes of each table
-      const int64_t at = row(axis);
-#pragma unroll
-      for (int j = 0; j < 8; j += 4) {
-        get<float, 4>(p.cos + at + j, c + j);
-        get<float, 4>(p.sin + at + j, s + j);
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        while (axis + 1 < p.axes && j0 + j >= p.end[axis]) ++axis;
-        const int64_t at = row(axis) + j;
-        c[j] = p.cos[at];
-        s[j] = p.sin[at];
-      }
-    }
-#pragma unroll
-    for (int k = 0; k < HEADS; ++k)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        float& lo = p.interleaved ? a[k][2 * j] : a[k][j];
-        float& hi = p.interleaved ? a[k][2 * j + 1] : a[k][8 + j];
-        const float x1 = lo, x2 = hi;
-        lo = x1 * c[j] - x2 * s[j];
-        hi = x2 * c[j] + x1 * s[j];
-      }
-  }
-#pragma unroll
-  for (int k = 0; k < HEADS; ++k) {
-    if (!o[k]) continue;
-#pragma unroll
-    for (int e = 0; e < 8; e += N) put<T, N, NT>(o[k] + at0 + e, a[k] + e);
-    if (turns)
-#pragma unroll
-      for (int e = 0; e < 8; e += N) put<T, N, NT>(o[k] + at1 + e, a[k] + 8 + e);
-  }
+  if (i < n) turn_heads<T, HEADS, NT>(p, t0, i);
 }
 
 template <typename T, int HEADS, bool NT> void rotary_launch(RotaryParams p, hipStream_t s) {
-  const int per = p.rot / 16 + (p.d - p.rot) / 8, groups = (p.heads[0] + p.heads[1] + HEADS - 1) / HEADS;
-  p.per_head = Divider(per);
-  p.per_token = Divider(per * groups);
+  set_threads<HEADS>(&p);
   // thread numbers stay below 2^31: more tokens than that take several launches
   const int64_t most = 0x7fffff00 / p.per_token.d;
   for (int64_t t0 = 0; t0 < p.T; t0 += most) {

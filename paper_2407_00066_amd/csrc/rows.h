@@ -1,0 +1,146 @@
+// Rows of elements in device code: 16-byte accesses, and the turning of a row's heads
+// by their positions (rownorm.hip, kvappend.hip).
+#pragma once
+
+#include "block_internal.h"
+
+namespace cts {
+namespace {
+
+template <typename T> struct Elem;
+template <> struct Elem<float> {
+  static constexpr int N = 4;                       // elements of 16 bytes
+  __device__ static __forceinline__ float get(const float* p) { return *p; }
+  __device__ static __forceinline__ void put(float* p, float v) { *p = v; }
+  __device__ static __forceinline__ void get16(const float* p, float* f) {
+    const float4 v = *reinterpret_cast<const float4*>(p);
+    f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w;
+  }
+  template <bool NT> __device__ static __forceinline__ void put16(float* p, const float* f) {
+    store16<NT>(p, __float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+  }
+};
+template <> struct Elem<bf16_t> {
+  static constexpr int N = 8;
+  __device__ static __forceinline__ float get(const bf16_t* p) { return bf16_to_f32(p->bits); }
+  __device__ static __forceinline__ void put(bf16_t* p, float v) { p->bits = f32_to_bf16(v); }
+  __device__ static __forceinline__ void get16(const bf16_t* p, float* f) {
+    const uint4 v = *reinterpret_cast<const uint4*>(p);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[2 * i] = __uint_as_float(w[i] << 16);
+      f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+  template <bool NT> __device__ static __forceinline__ void put16(bf16_t* p, const float* f) {
+    store16<NT>(p, f32_to_bf16_pair(f[0], f[1]), f32_to_bf16_pair(f[2], f[3]), f32_to_bf16_pair(f[4], f[5]),
+                f32_to_bf16_pair(f[6], f[7]));
+  }
+};
+
+// V consecutive elements: one 16-byte access, or one element
+template <typename T, int V> __device__ __forceinline__ void get(const T* p, float* f) {
+  if constexpr (V == 1) f[0] = Elem<T>::get(p);
+  else Elem<T>::get16(p, f);
+}
+template <typename T, int V, bool NT> __device__ __forceinline__ void put(T* p, const float* f) {
+  if constexpr (V == 1) Elem<T>::put(p, f[0]);
+  else Elem<T>::template put16<NT>(p, f);
+}
+
+// A pair turned by its angle; the same two instructions each wherever it is computed, so
+// that the calls that turn rows agree by bits.
+__device__ __forceinline__ void turn(float& lo, float& hi, float c, float s) {
+  const float x1 = lo, x2 = hi;
+  lo = __builtin_fmaf(x1, c, -(x2 * s));
+  hi = __builtin_fmaf(x2, c, x1 * s);
+}
+
+// Cosines and sines of token t's pairs j0 .. j0 + N - 1 (N 4 or 8, j0 a multiple of N).
+template <int N> __device__ __forceinline__ void angles(const RotaryParams& p, int64_t t, int j0, float* c, float* s) {
+  int axis = 0;
+  while (axis + 1 < p.axes && j0 >= p.end[axis]) ++axis;
+  auto row = [&](int ax) {
+    return static_cast<int64_t>(min(max(p.pos[static_cast<int64_t>(ax) * p.T + t], 0), p.n_pos - 1)) * (p.rot / 2) + j0;
+  };
+  if (j0 + N <= p.end[axis]) {                    // one axis: 16 or 32 bytes of each table
+    const int64_t at = row(axis);
+#pragma unroll
+    for (int j = 0; j < N; j += 4) {
+      get<float, 4>(p.cos + at + j, c + j);
+      get<float, 4>(p.sin + at + j, s + j);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      while (axis + 1 < p.axes && j0 + j >= p.end[axis]) ++axis;
+      const int64_t at = row(axis) + j;
+      c[j] = p.cos[at];
+      s[j] = p.sin[at];
+    }
+  }
+}
+
+// Thread `i` of the tokens from t0 on: it turns 8 pairs of a head (with halves, 8 elements of
+// each half; interleaved, 16 consecutive ones) or copies 8 elements past rot, for HEADS
+// heads that share the pairs' angles: their cosines and sines are loaded once for all of them.
+template <typename T, int HEADS, bool NT>
+__device__ __forceinline__ void turn_heads(const RotaryParams& p, int64_t t0, int i) {
+  constexpr int N = Elem<T>::N;
+  const int64_t t = t0 + p.per_token(i);
+  const int in_token = i - p.per_token(i) * p.per_token.d;
+  const int group = p.per_head(in_token), piece = in_token - group * p.per_head.d;
+  const int heads = p.heads[0] + p.heads[1], groups = (heads + HEADS - 1) / HEADS;
+  const int pieces = p.rot / 16, half = p.rot / 2;
+  const bool turns = piece < pieces;
+  const int j0 = piece * 8;                       // the first pair
+  const int at0 = !turns ? p.rot + (piece - pieces) * 8 : p.interleaved ? 2 * j0 : j0;
+  const int at1 = p.interleaved ? 2 * j0 + 8 : j0 + half;
+  float a[HEADS][16];
+  T* o[HEADS];
+#pragma unroll
+  for (int k = 0; k < HEADS; ++k) {
+    const int all = group + k * groups;
+    o[k] = nullptr;
+    if (all >= heads) continue;
+    const int which = all >= p.heads[0], head = which ? all - p.heads[0] : all;
+    const T* x = static_cast<const T*>(p.in[which]) + t * p.ldi[which] + static_cast<int64_t>(head) * p.d;
+    o[k] = static_cast<T*>(p.out[which]) + t * p.ldo[which] + static_cast<int64_t>(head) * p.d;
+#pragma unroll
+    for (int e = 0; e < 8; e += N) get<T, N>(x + at0 + e, a[k] + e);
+    if (turns)
+#pragma unroll
+      for (int e = 0; e < 8; e += N) get<T, N>(x + at1 + e, a[k] + 8 + e);
+  }
+  if (turns) {
+    float c[8], s[8];
+    angles<8>(p, t, j0, c, s);
+#pragma unroll
+    for (int k = 0; k < HEADS; ++k)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (p.interleaved) turn(a[k][2 * j], a[k][2 * j + 1], c[j], s[j]);
+        else turn(a[k][j], a[k][8 + j], c[j], s[j]);
+      }
+  }
+#pragma unroll
+  for (int k = 0; k < HEADS; ++k) {
+    if (!o[k]) continue;
+#pragma unroll
+    for (int e = 0; e < 8; e += N) put<T, N, NT>(o[k] + at0 + e, a[k] + e);
+    if (turns)
+#pragma unroll
+      for (int e = 0; e < 8; e += N) put<T, N, NT>(o[k] + at1 + e, a[k] + 8 + e);
+  }
+}
+
+// The threads of a head and of a token that turn_heads takes.
+template <int HEADS> void set_threads(RotaryParams* p) {
+  const int per = p->rot / 16 + (p->d - p->rot) / 8, groups = (p->heads[0] + p->heads[1] + HEADS - 1) / HEADS;
+  p->per_head = Divider(per);
+  p->per_token = Divider(per * groups);
+}
+
+}  // namespace
+}  // namespace cts
