@@ -12,11 +12,10 @@
 #include <algorithm>
 
 #include "attention_common.h"
+#include "ldsdma.h"
 
 namespace cts {
 namespace {
-
-constexpr int kMaskRow = kTreeMaxQ / 32 + 2;
 
 struct TreeTile {
   int b, q0, drafts, rows, row0;   // the sequence, its first query row, the drafts that count, its rows, the tile's first
@@ -50,6 +49,9 @@ __device__ __forceinline__ TreeTile uniform(TreeTile t) {
           __builtin_amdgcn_readfirstlane(t.steps)};
 }
 
+// The maximum of a row that has seen nothing: finite, so that no step asks whether there is one.
+constexpr float kNoMax = -3.0e38f;
+
 // What a wave holds of 16 rows (attention.hip).
 template <int D> struct Sums {
   static constexpr int NC = D > 128 ? 2 : 1;
@@ -62,11 +64,118 @@ template <int D> struct Sums {
   }
 };
 
-template <int D, int RG, int WAVES> struct TreeShared {
-  uint32_t mask[RG * kRowTile][kMaskRow];          // of the tile's queries
-  float sums[WAVES][kRowTile][D + 4];
-  float2 ml[WAVES][kRowTile];
+// Groups of 16 rows that a workgroup can take: what registers hold.
+constexpr int most_groups(int d, bool f32) { return d == 256 ? (f32 ? 1 : 2) : f32 ? 2 : 4; }
+
+// Parts of a query or weight in bf16, 16-byte pieces of its rows' queries that a lane multiplies, and whether
+// they stay in shared memory: more than 6 of them a lane leave too little room for the sums.
+template <int D, typename TQ, int RG> struct Query {
+  static constexpr int NS = sizeof(TQ) == 4 ? 3 : 1, KS = D / 32, N = RG * KS * NS;
+  static constexpr bool kShared = N > 6;
+  // words of a query's mask: a tile of fewer rows than the most has all of its sequence's
+  static constexpr int kMask = 2 + (RG == most_groups(D, sizeof(TQ) == 4) ? kTreeMaxQ / 32 : 1);
 };
+
+// A step's codes and scales, loaded straight into shared memory where the lane that loads
+// 16 bytes is, as a rule, the one that converts them: a wave's own, SLOTS steps
+// under way, no registers held and no barrier.
+template <int D> struct Step {
+  static constexpr int kPieces = D == 64 ? 1 : D / 64;       // loads of 16 bytes a lane for the keys, as many for the values
+  static constexpr int kScales = D == 256 ? 2 : 1;           // loads of 4 bytes a lane for the scales
+  static constexpr int kLoads = 2 * kPieces + kScales;
+  static constexpr int kBytes = 2 * kPieces * 1024 + kScales * 256;
+  static constexpr int kSlots = 2;
+};
+
+// Shared memory.  Queries and masks stand in arrays of their own: the compiler waits for all loads
+// under way before it reads from the array that they go to, and not before others.
+template <int D, int WAVES> union Codes {
+  char ring[WAVES][Step<D>::kSlots][Step<D>::kBytes];
+  struct {
+    float sums[WAVES][kRowTile][D + 4];
+    float2 ml[WAVES][4 * kRowTile];
+  } done;
+};
+
+__device__ __forceinline__ uint32_t lds_at(const void* p) {
+  return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void*)p));
+}
+// Each lane's 16 or 4 bytes at `base` (the same for the whole wave) + off, to lds + 16 or 4 x lane.
+__device__ __forceinline__ void load_lds16(const uint8_t* base, uint32_t off, char* lds) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void*)(base + off),
+                                   (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
+#endif
+}
+__device__ __forceinline__ void load_lds4(const uint8_t* at, char* lds) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void*)at,
+                                   (__attribute__((address_space(3))) void*)lds, 4, 0, 0);
+#endif
+}
+
+// A step's keys and their scales of both groups of 16 tokens, from shared memory: reads and their wait in
+// one piece of assembly (as plain reads they would wait for the next step's loads too).
+// at: the step; k: KS words of each group, ks: scales of the lane's elements.
+template <int D> __device__ __forceinline__ void read_keys(uint32_t at, int lane, uint32_t (*k)[D / 32], uint32_t* ks) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const int n = lane & 15, g = lane >> 4;
+  if constexpr (D == 64) {
+    uint64_t a, b;
+    asm volatile("ds_read_b64 %0, %4\n\tds_read_b64 %1, %4 offset:512\n\tds_read_u8 %2, %5 offset:2048\n\t"
+                 "ds_read_u8 %3, %5 offset:2080\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(a), "=&v"(b), "=&v"(ks[0]), "=&v"(ks[1]) : "v"(at + n * 32 + g * 8), "v"(at + n * 2 + (g >> 1)) : "memory");
+    k[0][0] = static_cast<uint32_t>(a); k[0][1] = static_cast<uint32_t>(a >> 32);
+    k[1][0] = static_cast<uint32_t>(b); k[1][1] = static_cast<uint32_t>(b >> 32);
+  } else if constexpr (D == 128) {
+    u32x4 a, b;
+    asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %4 offset:1024\n\tds_read_u8 %2, %5 offset:4096\n\t"
+                 "ds_read_u8 %3, %5 offset:4160\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(a), "=&v"(b), "=&v"(ks[0]), "=&v"(ks[1]) : "v"(at + lane * 16), "v"(at + n * 4 + g) : "memory");
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { k[0][i] = a[i]; k[1][i] = b[i]; }
+  } else {
+    u32x4 a, b, c, d;
+    asm volatile("ds_read_b128 %0, %6\n\tds_read_b128 %1, %6 offset:1024\n\tds_read_b128 %2, %6 offset:2048\n\t"
+                 "ds_read_b128 %3, %6 offset:3072\n\tds_read_u16 %4, %7 offset:8192\n\tds_read_u16 %5, %7 offset:8320\n\t"
+                 "s_waitcnt lgkmcnt(0)"
+                 : "=&v"(a), "=&v"(b), "=&v"(c), "=&v"(d), "=&v"(ks[0]), "=&v"(ks[1])
+                 : "v"(at + lane * 16), "v"(at + n * 8 + 2 * g) : "memory");
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { k[0][i] = a[i]; k[0][4 + i] = b[i]; k[1][i] = c[i]; k[1][4 + i] = d[i]; }
+  }
+#endif
+}
+
+// The step's values: v, 8 elements of 4 tokens a piece, and their tokens' scales.
+template <int D> __device__ __forceinline__ void read_values(uint32_t at, int lane, uint32_t (*v)[D > 128 ? 2 : 1][4],
+                                                             uint32_t (*vs)[D > 128 ? 2 : 1]) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const int n = lane & 15, g = lane >> 4;
+  if constexpr (D <= 128) {
+    // (heads of 64: lanes n and n + 8 read the same piece)
+    constexpr int kAt = D == 64 ? 1024 : 2048, kStep = D == 64 ? 512 : 1024, kScale = D == 64 ? 2048 + 64 : 4096 + 128;
+    const uint32_t from = at + (D == 64 ? (g * 8 + (n & 7)) * 16 : lane * 16);
+    const uint32_t scale = at + (D == 64 ? (g * 2 + ((n & 7) >> 2)) * 4 : (g * 4 + (n >> 2)) * 4);
+    u32x4 a, b;
+    asm volatile("ds_read_b128 %0, %4 offset:%6\n\tds_read_b128 %1, %4 offset:%7\n\tds_read_b32 %2, %5 offset:%8\n\t"
+                 "ds_read_b32 %3, %5 offset:%9\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(a), "=&v"(b), "=&v"(vs[0][0]), "=&v"(vs[1][0])
+                 : "v"(from), "v"(scale), "n"(kAt), "n"(kAt + kStep), "n"(kScale), "n"(kScale + D / 2) : "memory");
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { v[0][0][i] = a[i]; v[1][0][i] = b[i]; }
+  } else {
+    u32x4 a, b, c, d;
+    asm volatile("ds_read_b128 %0, %8 offset:4096\n\tds_read_b128 %1, %8 offset:5120\n\tds_read_b128 %2, %8 offset:6144\n\t"
+                 "ds_read_b128 %3, %8 offset:7168\n\tds_read_b32 %4, %9 offset:8448\n\tds_read_b32 %5, %9 offset:8464\n\t"
+                 "ds_read_b32 %6, %9 offset:8576\n\tds_read_b32 %7, %9 offset:8592\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(a), "=&v"(b), "=&v"(c), "=&v"(d), "=&v"(vs[0][0]), "=&v"(vs[0][1]), "=&v"(vs[1][0]), "=&v"(vs[1][1])
+                 : "v"(at + lane * 16), "v"(at + (g * 8 + (n >> 2)) * 4) : "memory");
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { v[0][0][i] = a[i]; v[0][1][i] = b[i]; v[1][0][i] = c[i]; v[1][1][i] = d[i]; }
+  }
+#endif
+}
 
 // Page number of the lane's group of 16 tokens in the steps s0, s0 + stride, ..: two
 // groups a step, a lane one.
@@ -76,184 +185,275 @@ __device__ __forceinline__ int look_up(const TreeParams& p, int b, int lo, int s
   return p.table[static_cast<int64_t>(b) * p.max_pages + min(tok >> p.c.page_shift, static_cast<int64_t>(p.max_pages - 1))];
 }
 
-// The bits of the tile's queries, into shared memory; those of drafts that do not count are 0.
-template <int ROWS> __device__ __forceinline__ void load_masks(const TreeParams& p, const TreeTile& t, uint32_t (*mask)[kMaskRow]) {
-  const int first = t.row0 / p.group, last = (min(t.rows, t.row0 + ROWS) - 1) / p.group;
-  const int words = (t.drafts + 31) / 32, wide = words + 2;
-  for (int k = threadIdx.x; k < (last - first + 1) * wide; k += blockDim.x) {
-    const int q = k / wide, w = k - q * wide - 1;
-    uint32_t bits = w < 0 ? ~0u : 0u;
-    if (w >= 0 && w < words) {
-      bits = p.mask[static_cast<int64_t>(t.q0 + first + q) * p.mask_words + w];
-      const int left = t.drafts - 32 * w;
-      if (left < 32) bits &= (1u << left) - 1;
-    }
-    mask[q][w + 1] = bits;
-  }
+// Word w of the tile's query q as it stands in shared memory: drafts that do not count are 0.
+__device__ __forceinline__ uint32_t mask_word(const TreeParams& p, const TreeTile& t, int first, int q, int w) {
+  if (w < 0) return ~0u;
+  const int left = t.drafts - 32 * w;
+  if (left <= 0) return 0;
+  const uint32_t bits = p.mask[static_cast<int64_t>(t.q0 + first + q) * p.mask_words + w];
+  return left < 32 ? bits & ((1u << left) - 1) : bits;
 }
 
-// `count` of the tile's steps from s0, `stride` apart, for key/value head h, by one
-// wave; pages: look_up of the first 32.  The workgroup meets once, for the masks.
-template <int D, typename TQ, int RG, int stride>
-__device__ __forceinline__ void attend(const TreeParams& p, const TreeTile& t, int h, int s0, int count, int pages,
-                                       uint32_t (*mask)[kMaskRow], Sums<D>* st) {
-  constexpr int NS = sizeof(TQ) == 4 ? 3 : 1;      // bf16 parts of a query and of a weight
-  constexpr int KS = D / 32;                     // steps of the first product; words of keys a lane holds
+// 32 bytes from `at` and from 1, 2 and 3 times STRIDE further on, added element by element to f (in one piece with
+// their wait: plain reads would wait for the stores under way).
+template <int STRIDE> __device__ __forceinline__ void add_four(uint32_t at, float* f) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  f32x4 v[8];
+  asm volatile("ds_read_b128 %0, %8\n\tds_read_b128 %1, %8 offset:16\n\tds_read_b128 %2, %8 offset:%9\n\t"
+               "ds_read_b128 %3, %8 offset:%10\n\tds_read_b128 %4, %8 offset:%11\n\tds_read_b128 %5, %8 offset:%12\n\t"
+               "ds_read_b128 %6, %8 offset:%13\n\tds_read_b128 %7, %8 offset:%14\n\ts_waitcnt lgkmcnt(0)"
+               : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]), "=&v"(v[4]), "=&v"(v[5]), "=&v"(v[6]), "=&v"(v[7])
+               : "v"(at), "n"(STRIDE), "n"(STRIDE + 16), "n"(2 * STRIDE), "n"(2 * STRIDE + 16), "n"(3 * STRIDE), "n"(3 * STRIDE + 16)
+               : "memory");
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      f[i] += v[2 * w][i];
+      f[4 + i] += v[2 * w + 1][i];
+    }
+#endif
+}
+
+// `count` of the tile's steps from s0, `stride` apart, for key/value head h, by
+// wave `wave`; pages: look_up of the first 32.  The workgroup meets once, for masks and queries.
+template <int D, typename TQ, int RG, int stride, int WIDE>
+__device__ __forceinline__ void attend(const TreeParams& p, const TreeTile& t, int h, int wave, int s0, int count, int pages,
+                                       Codes<D, stride>& codes, bf16x8 (*queries)[64], uint32_t (*masks)[WIDE], int2* seers, Sums<D>* st) {
+  using Q = Query<D, TQ, RG>;
+  using S = Step<D>;
+  constexpr int NS = Q::NS, KS = Q::KS;          // (KS: steps of the first product; words of keys a lane holds)
   constexpr int NC = Sums<D>::NC, NB = Sums<D>::NB;
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-
-  struct Group { int64_t base; uint32_t bad; };       // a group's first token among its head's; all ones: its page is outside the cache
-  const int page_mask = (1 << p.c.page_shift) - 1;
-  auto group_of = [&](int it, int i) -> Group {
-    const int page = __builtin_amdgcn_readlane(pages, 2 * (it & 31) + i);
-    const int tok = t.lo + (s0 + it * stride) * kUnit + 16 * i;
-    const bool bad = static_cast<uint32_t>(page) >= static_cast<uint32_t>(p.c.n_pages);
-    return {((static_cast<int64_t>(bad ? 0 : page) * p.c.heads + h) << p.c.page_shift) + (tok & page_mask), bad ? ~0u : 0u};
-  };
-  const uint32_t k_at = n * (D / 2) + g * (D / 8), ks_at = n * (D / 32) + (D == 64 ? g >> 1 : D == 128 ? g : 2 * g);
-  uint32_t v_at[NC], vs_at[NC];
-#pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    const int eighth = (n & (D / 8 - 1)) + 16 * c;
-    v_at[c] = (g * (D / 8) + eighth) * 16;
-    vs_at[c] = (g * (D / 32) + eighth / 4) * 4;
-  }
-  uint32_t k[2][KS], ks[2], vs[2][NC], v_bad[2];
-  uint4 v[2][NC];
-  Group gr[2];
-  auto load_k = [&](int it) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      gr[i] = group_of(it, i);
-      const uint8_t* kc = p.c.kc + gr[i].base * (D / 2);
-      const uint8_t* sc = p.c.ks + gr[i].base * (D / 32);
-      if constexpr (D == 64) {
-        const uint2 w = *reinterpret_cast<const uint2*>(kc + k_at);
-        k[i][0] = w.x; k[i][1] = w.y;
-      } else {
-#pragma unroll
-        for (int x = 0; x < D / 128; ++x) {
-          const uint4 w = *reinterpret_cast<const uint4*>(kc + k_at + 16 * x);
-          k[i][4 * x] = w.x; k[i][4 * x + 1] = w.y; k[i][4 * x + 2] = w.z; k[i][4 * x + 3] = w.w;
-        }
-      }
-      ks[i] = D == 256 ? *reinterpret_cast<const uint16_t*>(sc + ks_at) : sc[ks_at];
-    }
-  };
-  auto load_v = [&]() {                                                  // of the step load_k was last called for
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint8_t* vc = p.c.vc + gr[i].base * (D / 2);
-      const uint8_t* sc = p.c.vs + gr[i].base * (D / 32);
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        v[i][c] = *reinterpret_cast<const uint4*>(vc + v_at[c]);
-        vs[i][c] = *reinterpret_cast<const uint32_t*>(sc + vs_at[c]);
-      }
-      v_bad[i] = gr[i].bad;
-    }
-  };
   const bool any = count > 0 && t.hi > t.lo;
-  if (any) {
-    load_k(0);
-    load_v();
-  }
 
-  // the lane's rows: which bits are theirs, and the first token before the drafts that they see
-  int q_of[RG], first[RG];
-  bf16x8 qf[RG][KS][NS];
+  // Of each group of 16 tokens a lane loads the 16 bytes that it converts: of keys token n,
+  // elements (D / 4) g on; of values quad g, eighth n (+ 16).  Heads of 64 have half as many bytes:
+  // a lane loads for both groups at once, and they are dealt out when they are read.
+  uint32_t k_at[S::kPieces], v_at[S::kPieces];
+  uint32_t s_at;
+  if constexpr (D == 64) {
+    k_at[0] = v_at[0] = (lane & 31) * 16;
+    s_at = (lane & 7) * 4;
+  } else {
+#pragma unroll
+    for (int c = 0; c < D / 128; ++c) {
+      k_at[c] = n * (D / 2) + g * (D / 8) + 16 * c;
+      v_at[c] = (g * (D / 8) + n + 16 * c) * 16;
+    }
+    s_at = (lane & (D / 8 - 1)) * 4;
+  }
+  char (*const ring)[S::kBytes] = codes.ring[wave];
+  const int page_mask = (1 << p.c.page_shift) - 1;
+  uint32_t bad = 0;                                // which groups of the last steps asked for lie outside the cache, two bits a step
+  int slot_in = 0, slot = 0;
+  auto ask = [&](int it) {                         // for step `it`, of which `pages` has the pages
+    int64_t base[2];
+    bad <<= 2;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int page = __builtin_amdgcn_readlane(pages, 2 * (it & 31) + i);
+      const int tok = t.lo + (s0 + it * stride) * kUnit + 16 * i;
+      const bool outside = static_cast<uint32_t>(page) >= static_cast<uint32_t>(p.c.n_pages);
+      bad |= outside ? 1u << i : 0u;
+      base[i] = ((static_cast<int64_t>(outside ? 0 : page) * p.c.heads + h) << p.c.page_shift) + (tok & page_mask);
+    }
+    char* to = ring[slot_in];
+    slot_in = slot_in + 1 == S::kSlots ? 0 : slot_in + 1;
+    if constexpr (D == 64) {
+      // (lanes 32 on: the second group)
+      const int64_t from = lane < 32 ? base[0] : base[1];
+      load_lds16(p.c.kc + from * 32, k_at[0], to);
+      load_lds16(p.c.vc + from * 32, v_at[0], to + 1024);
+      const int which = lane >> 3 & 3;             // (lanes 32 on load the same once more)
+      const int64_t of = which & 1 ? base[1] : base[0];
+      load_lds4((which & 2 ? p.c.vs : p.c.ks) + of * 2 + s_at, to + 2048);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int c = 0; c < D / 128; ++c) {
+          load_lds16(p.c.kc + base[i] * (D / 2), k_at[c], to);
+          to += 1024;
+        }
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int c = 0; c < D / 128; ++c) {
+          load_lds16(p.c.vc + base[i] * (D / 2), v_at[c], to);
+          to += 1024;
+        }
+      if constexpr (D == 128) {
+        const int which = lane >> 4;
+        const int64_t of = which & 1 ? base[1] : base[0];
+        load_lds4((which & 2 ? p.c.vs : p.c.ks) + of * 4 + s_at, to);
+      } else {
+        const int64_t of = lane & 32 ? base[1] : base[0];
+        load_lds4(p.c.ks + of * 8 + s_at, to);
+        load_lds4(p.c.vs + of * 8 + s_at, to + 256);
+      }
+    }
+  };
+  // All that is needed is asked for before any of it is waited for: the masks' first words, the queries, then the codes.
+  const int q_first = p.by_group(t.row0), q_last = p.by_group(min(t.rows, t.row0 + RG * kRowTile) - 1);
+  const int words = (q_last - q_first + 1) * WIDE;
+  uint32_t word = 0;
+  if (static_cast<int>(threadIdx.x) < words) word = mask_word(p, t, q_first, threadIdx.x / WIDE, static_cast<int>(threadIdx.x % WIDE) - 1);
+  bf16x8 qf[Q::kShared ? 1 : RG][KS][NS];
+  auto query_at = [&](int r, bool* live) -> const TQ* {
+    const int row = t.row0 + kRowTile * r + n, query = p.by_group(row);
+    *live = row < t.rows;
+    return static_cast<const TQ*>(p.q) + (*live ? (t.q0 + query) * p.ldq +
+                                          static_cast<int64_t>(h * p.group + row - query * p.group) * D : 0) + (D / 4) * g;
+  };
+  constexpr int kMine = Q::kShared ? (RG * KS + stride - 1) / stride : RG * KS;      // the waves share out what they share
+  float f[kMine][8];
+#pragma unroll
+  for (int k = 0; k < kMine; ++k) {
+    const int i = Q::kShared ? wave + k * stride : k, r = i / KS, s = i - r * KS;
+    bool live;
+    const TQ* const q = query_at(min(r, RG - 1), &live);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[k][e] = 0.0f;
+    if (live) load_q(q + 8 * s, f[k]);
+  }
+  // of row `lane`: its query's place among the tile's, and the first token before the drafts that it sees
+  int2 seer = make_int2(0, 0);
+  {
+    const int row = min(t.row0 + lane, t.rows - 1), query = p.by_group(row);
+    seer.x = query - q_first;
+    if (p.window) seer.y = min(max(p.positions[t.q0 + query], t.past) - p.window + 1, t.past);
+  }
+  if (any)
+#pragma unroll
+    for (int i = 0; i < S::kSlots - 1; ++i) ask(min(i, count - 1));
+  for (int k = threadIdx.x; k < words; k += 64 * stride) {
+    if (k >= 64 * stride) word = mask_word(p, t, q_first, k / WIDE, k % WIDE - 1);
+    masks[k / WIDE][k % WIDE] = word;
+  }
+  if (threadIdx.x < RG * kRowTile) seers[threadIdx.x] = seer;           // (the first wave's)
+#pragma unroll
+  for (int k = 0; k < kMine; ++k) {
+    if constexpr (Q::kShared) {
+      const int i = wave + k * stride;
+      bf16x8 part[NS];
+      split<NS>(f[k], part);
+      if (i < RG * KS)
+#pragma unroll
+        for (int z = 0; z < NS; ++z) queries[i * NS + z][lane] = part[z];
+    } else {
+      split<NS>(f[k], qf[k / KS][k % KS]);
+    }
+  }
 #pragma unroll
   for (int r = 0; r < RG; ++r) {
-    const int row = t.row0 + kRowTile * r + n;
-    const bool live = row < t.rows;
-    const int query = (live ? row : t.row0) / p.group;
-    q_of[r] = query - t.row0 / p.group;
-    first[r] = p.window && live ? min(max(p.positions[t.q0 + query], t.past) - p.window + 1, t.past) : 0;
-    const TQ* q = static_cast<const TQ*>(p.q) + (live ? (t.q0 + query) * p.ldq +
-                                                 static_cast<int64_t>(h * p.group + row - query * p.group) * D : 0);
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      float f[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-      if (live) load_q(q + (D / 4) * g + 8 * s, f);
-      split<NS>(f, qf[r][s]);
-    }
 #pragma unroll
     for (int c = 0; c < NC; ++c)
 #pragma unroll
       for (int e = 0; e < NB; ++e) st[r].o[c][e] = f32x4{0, 0, 0, 0};
-    st[r].m = -INFINITY;
+    st[r].m = kNoMax;
     st[r].l = 0.0f;
   }
   // tokens from here on every row sees, as far as windows go
   int all_lo = 0;
   if (p.window) {
+    all_lo = max(0, seer.y);
 #pragma unroll
-    for (int r = 0; r < RG; ++r) all_lo = max(all_lo, first[r]);
-#pragma unroll
-    for (int x = 1; x < 16; x <<= 1) all_lo = max(all_lo, __shfl_xor(all_lo, x));
+    for (int x = 1; x < 64; x <<= 1) all_lo = max(all_lo, __shfl_xor(all_lo, x));
     all_lo = __builtin_amdgcn_readfirstlane(all_lo);
   }
-  __syncthreads();                                                      // the masks are there
+  lds_barrier();                                                        // masks and queries are there
   if (!any) return;
 
+  pages = rare(pages);                             // here: waited for inside the loop, the loads under way would be too
+  const uint32_t ring_at = __builtin_amdgcn_readfirstlane(lds_at(ring));
   for (int it = 0; it < count; ++it) {
     const int at = t.lo + (s0 + it * stride) * kUnit;
+    // the next step's codes are asked for (past the end: the last step's again); this one's have to be there
+    const int next = min(it + S::kSlots - 1, count - 1);
+    if ((next & 31) == 0 && next != 0) pages = rare(look_up(p, t.b, t.lo, s0 + next * stride, stride));
+    ask(next);
+    wait_vmcnt<(S::kSlots - 1) * S::kLoads>();
+    const uint32_t from = ring_at + slot * S::kBytes;
+    slot = slot + 1 == S::kSlots ? 0 : slot + 1;
+    const uint32_t bad_now = bad >> (2 * (S::kSlots - 1));
+
     // scores of the lane's rows against tokens at + 16 i + 4 g + j
     f32x4 x[RG][2];
+    {
+      uint32_t k[2][KS], ks[2];
+      read_keys<D>(from, lane, k, ks);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+      for (int i = 0; i < 2; ++i) {
+        if (bad_now >> i & 1) ks[i] = ~0u;
 #pragma unroll
-      for (int r = 0; r < RG; ++r) x[r][i] = f32x4{0, 0, 0, 0};
-      const uint32_t units = ks[i] | gr[i].bad;                          // here: asked for sooner, it would be waited for sooner
+        for (int r = 0; r < RG; ++r) x[r][i] = f32x4{0, 0, 0, 0};
+      }
 #pragma unroll
       for (int y = 0; y < KS; ++y) {
-        const float unit = unit_of(units, D == 256 ? y / 4 : 0);
-        const bf16x8 a = frag(fp4_pair(k[i][y], unit, 0), fp4_pair(k[i][y], unit, 1),
-                              fp4_pair(k[i][y], unit, 2), fp4_pair(k[i][y], unit, 3));
+        bf16x8 a[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float unit = unit_of(ks[i], D == 256 ? y / 4 : 0);
+          a[i] = frag(fp4_pair(k[i][y], unit, 0), fp4_pair(k[i][y], unit, 1), fp4_pair(k[i][y], unit, 2), fp4_pair(k[i][y], unit, 3));
+        }
 #pragma unroll
         for (int r = 0; r < RG; ++r)
 #pragma unroll
-          for (int z = 0; z < NS; ++z) x[r][i] = mfma(a, qf[r][y][z], x[r][i]);
+          for (int z = 0; z < NS; ++z) {
+            const bf16x8 b = Q::kShared ? queries[Q::kShared ? (r * KS + y) * NS + z : 0][lane] : qf[Q::kShared ? 0 : r][y][z];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) x[r][i] = mfma(a[i], b, x[r][i]);
+          }
       }
     }
-    // the next keys are on their way during the softmax and the second product,
-    // the next values during the next first product (past the end: the last step's again)
-    const int next = min(it + 1, count - 1);
-    if ((next & 31) == 0 && next != 0) pages = rare(look_up(p, t.b, t.lo, s0 + next * stride, stride));
-    load_k(next);
+    uint32_t v[2][NC][4], vs[2][NC];
+    read_values<D>(from, lane, v, vs);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+        if (bad_now >> i & 1) vs[i][c] = ~0u;
 
     const bool masked = at + kUnit > t.past || at < all_lo;              // the same for the whole wave
     // which of tokens at + 4 g .. a row sees (bit 16 i + j)
     auto seen_by = [&](int r) -> uint32_t {
-      const int from = rare(max(at - t.past, -kUnit));
-      const uint32_t* const w = &mask[q_of[r]][(from >> 5) + 1];
-      uint32_t bits = static_cast<uint32_t>((static_cast<uint64_t>(w[1]) << 32 | w[0]) >> (from & 31));
-      const int hide = first[r] - at;                                    // tokens that a window hides
+      const int begin = rare(max(at - t.past, -kUnit));
+      const int2 seer = seers[kRowTile * r + n];
+      const uint32_t* const w = &masks[seer.x][(begin >> 5) + 1];
+      uint32_t bits = static_cast<uint32_t>((static_cast<uint64_t>(w[1]) << 32 | w[0]) >> (begin & 31));
+      const int hide = seer.y - at;                                      // tokens that a window hides
       if (hide > 0) bits &= hide < 32 ? ~0u << hide : 0u;
       return bits >> (4 * g);
     };
-    bf16x8 pf[RG][NS];
+    if (masked) {
 #pragma unroll
-    for (int r = 0; r < RG; ++r) {
-      float sc[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) sc[i] = x[r][i >> 2][i & 3] * p.scale_log2e;
-      if (masked) {
+      for (int r = 0; r < RG; ++r) {
         const uint32_t bits = seen_by(r);
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            if (!(bits >> (16 * i + j) & 1)) sc[4 * i + j] = -INFINITY;
+            if (!(bits >> (16 * i + j) & 1)) x[r][i][j] = -INFINITY;
       }
-      float top = sc[0];
+    }
+    // The maxima are looked at lane by lane, and across lanes only where one has grown past the slack.
+    auto top_of = [&](int r) {
+      float top = x[r][0][0];
 #pragma unroll
-      for (int i = 1; i < 8; ++i) top = fmaxf(top, sc[i]);
-      top = max_over_groups(top);
-      if (__any(top > st[r].m + kSlack)) {
+      for (int i = 1; i < 8; ++i) top = fmaxf(top, x[r][i >> 2][i & 3]);
+      return top * p.scale_log2e;
+    };
+    bool grown = false;
+#pragma unroll
+    for (int r = 0; r < RG; ++r) grown |= top_of(r) > st[r].m + kSlack;
+    if (__any(grown)) {
+#pragma unroll
+      for (int r = 0; r < RG; ++r) {
         // (only the rows that have grown follow, so that no row's bits depend on another's)
-        const float m_new = top > st[r].m + kSlack ? top : st[r].m;
-        const float fade = __builtin_amdgcn_exp2f(st[r].m - (m_new == -INFINITY ? 0.0f : m_new));
+        const float all = max_over_groups(top_of(r));
+        const float m_new = all > st[r].m + kSlack ? all : st[r].m;
+        const float fade = __builtin_amdgcn_exp2f(st[r].m - m_new);
         st[r].l *= fade;
 #pragma unroll
         for (int c = 0; c < NC; ++c)
@@ -261,11 +461,14 @@ __device__ __forceinline__ void attend(const TreeParams& p, const TreeTile& t, i
           for (int e = 0; e < NB; ++e) st[r].o[c][e] *= fade;
         st[r].m = m_new;
       }
-      const float base = st[r].m == -INFINITY ? 0.0f : st[r].m;
+    }
+    bf16x8 pf[RG][NS];
+#pragma unroll
+    for (int r = 0; r < RG; ++r) {
       float w[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        w[i] = __builtin_amdgcn_exp2f(sc[i] - base);
+        w[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r][i >> 2][i & 3], p.scale_log2e, -st[r].m));
         if (NS == 3) st[r].l += w[i];
       }
       split<NS>(w, pf[r]);
@@ -278,8 +481,6 @@ __device__ __forceinline__ void attend(const TreeParams& p, const TreeTile& t, i
 
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-      vs[0][c] |= v_bad[0];
-      vs[1][c] |= v_bad[1];
       if (masked) {
         // A weight of zero does not hide a NaN or infinite value: blocks that can hold one are
         // taken out of the product, and the rows that do see one are made NaN.
@@ -296,7 +497,7 @@ __device__ __forceinline__ void attend(const TreeParams& p, const TreeTile& t, i
             for (int j = 0; j < 4; ++j)
               if (past_scales(vs[i][c], j)) {
                 vs[i][c] ^= 0x80u << (8 * j);                            // 255 -> 127
-                (&v[i][c].x)[j] = 0;
+                v[i][c][j] = 0;
               }
 #pragma unroll
           for (int r = 0; r < RG; ++r) {
@@ -317,7 +518,6 @@ __device__ __forceinline__ void attend(const TreeParams& p, const TreeTile& t, i
           }
         }
       }
-      const uint32_t* vw[2] = {&v[0][c].x, &v[1][c].x};
 #pragma unroll
       for (int e = 0; e < NB / 2; ++e) {
         uint32_t y[2][4];
@@ -325,7 +525,7 @@ __device__ __forceinline__ void attend(const TreeParams& p, const TreeTile& t, i
         for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            y[i][j] = fp4_pair(D == 64 ? vw[i][j] >> (16 * (n >> 3)) : vw[i][j], unit_of(vs[i][c], j), e);
+            y[i][j] = fp4_pair(D == 64 ? v[i][c][j] >> (16 * (n >> 3)) : v[i][c][j], unit_of(vs[i][c], j), e);
         const bf16x8 even = frag(__builtin_amdgcn_perm(y[0][1], y[0][0], 0x05040100u), __builtin_amdgcn_perm(y[0][3], y[0][2], 0x05040100u),
                                  __builtin_amdgcn_perm(y[1][1], y[1][0], 0x05040100u), __builtin_amdgcn_perm(y[1][3], y[1][2], 0x05040100u));
         const bf16x8 odd = frag(__builtin_amdgcn_perm(y[0][1], y[0][0], 0x07060302u), __builtin_amdgcn_perm(y[0][3], y[0][2], 0x07060302u),
@@ -339,92 +539,342 @@ __device__ __forceinline__ void attend(const TreeParams& p, const TreeTile& t, i
           }
       }
     }
-    load_v();
   }
 #pragma unroll
   for (int r = 0; r < RG; ++r) st[r].l = sum_over_groups(st[r].l);
+  wait_vmcnt<0>();                                                      // the last loads, whatever they bring
 }
 
-// Eight elements of a row, from e: the waves' sums together, their maximum and length.
-template <int D, int RG, int WAVES>
-__device__ __forceinline__ float2 join_waves(const TreeShared<D, RG, WAVES>& sh, int r, int e, float* f) {
-  float M = -INFINITY;
-#pragma unroll
-  for (int v = 0; v < WAVES; ++v) M = fmaxf(M, sh.ml[v][r].x);
-  const float base = M == -INFINITY ? 0.0f : M;
-  float L = 0.0f;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) f[i] = 0.0f;
-#pragma unroll
-  for (int v = 0; v < WAVES; ++v) {
-    const float2 w = sh.ml[v][r];
-    if (w.y == 0.0f) continue;                     // saw nothing: no sums
-    const float a = __builtin_amdgcn_exp2f(w.x - base);
-    L += a * w.y;
-    const float4* o = reinterpret_cast<const float4*>(&sh.sums[v][r][e]);
-    const float4 x = o[0], y = o[1];
-    f[0] += a * x.x; f[1] += a * x.y; f[2] += a * x.z; f[3] += a * x.w;
-    f[4] += a * y.x; f[5] += a * y.y; f[6] += a * y.z; f[7] += a * y.w;
+// What a workgroup takes: some steps of a tile for one head, and where their sums go if that is not all of them.
+struct Piece {
+  TreeTile t;
+  int h, begin, end, slot;
+};
+
+// Work is counted in units of about 150 cycles: a step takes 2 and one for every group of rows.
+__device__ __forceinline__ int unit_of(const TreeTile& t, int tile_rows) {
+  return 2 + (min(t.rows - t.row0, tile_rows) + kRowTile - 1) / kRowTile;
+}
+
+__device__ __forceinline__ TreeTile tile_at(const TreeParams& p, int i) {
+  const int b = p.subs == 1 ? i : i / p.subs;
+  return tree_tile(p, b, i - b * p.subs);
+}
+
+// Piece w of the batch; false: there are not so many.  As long as there are no more tiles than workgroups that run
+// at a time, they are cut along their tokens into equal pieces until there are as many of those; of more tiles,
+// those whose work is past twice a workgroup's share of all.  Up to 64 tiles (of a head) are taken by the length
+// of their pieces, to an eighth: the longest first, one to a compute unit, then the shortest beside
+// them, then the others as workgroups end.
+__device__ __forceinline__ bool find_piece(const TreeParams& p, int w, Piece* out) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tiles = p.B * p.subs;
+  int4* const info = reinterpret_cast<int4*>(p.info);
+  TreeTile t0{};                                     // the first 64 are kept
+  int total = 0, some = 0;                           // units, tiles that have any
+  for (int base = 0; base < tiles; base += 64) {
+    const int i = base + lane;
+    TreeTile t{};
+    if (i < tiles) t = tile_at(p, i);
+    if (i < tiles && t.steps == 0 && i % static_cast<int>(gridDim.x) == w && wave == 0)
+      for (int h = 0; h < p.c.heads; ++h) info[static_cast<int64_t>(i) * p.c.heads + h] = make_int4(0, 0, 0, 0);
+    if (base == 0) t0 = t;
+    total += __builtin_amdgcn_readlane(wave_scan(t.steps * unit_of(t, p.tile_rows)), 63);
+    some += __builtin_popcountll(__ballot(t.steps > 0));
   }
-  return make_float2(M, L);
+  total *= p.c.heads;
+  some *= p.c.heads;
+  if (total == 0) return false;
+  const bool few = some <= p.resident && tiles <= 64;
+  int len = max(p.least, (few ? 1 : 2) * ((total - 1) / p.resident + 1));
+  auto pieces_of = [&](const TreeTile& t) {
+    const int units = t.steps * unit_of(t, p.tile_rows);
+    return units <= len ? (units > 0 ? 1 : 0) : static_cast<int>(static_cast<float>(units) * __builtin_amdgcn_rcpf(static_cast<float>(len))) + 1;
+  };
+  int at = 0, base = 0, of = 0, mine = 0;            // the tile, and the piece's number among its heads' pieces
+  TreeTile t = t0;
+  if (tiles <= 64) {
+    int n;
+    for (;; len += len / 16 + 1) {
+      mine = pieces_of(t);
+      n = __builtin_amdgcn_readlane(wave_scan(mine), 63) * p.c.heads;
+      if (!few || n <= p.resident) break;
+    }
+    if (w >= n) return false;
+    const int beside = p.resident - 256;             // (workgroups that have a place beside another)
+    of = w < 256 ? w : w < 256 + beside ? n - 1 - (w - 256) : w - beside;
+    const int bucket = mine ? min(7, static_cast<int>(static_cast<float>(t.steps * unit_of(t, p.tile_rows)) *
+                                                      __builtin_amdgcn_rcpf(static_cast<float>(mine * len)) * 8.0f)) : -1;
+    int before = 0;                                  // pieces that come first
+#pragma unroll
+    for (int k = 7, all = 0; k >= 0; --k) {
+      const int v = bucket == k ? mine : 0, to = wave_scan(v);
+      if (bucket == k) before = all + to - v;
+      all += __builtin_amdgcn_readlane(to, 63);
+    }
+    at = __builtin_ctzll(__ballot(before * p.c.heads <= of && of < (before + mine) * p.c.heads));
+    out->slot = of;
+    of -= __builtin_amdgcn_readlane(before, at) * p.c.heads;
+  } else {
+    uint64_t here = 0;
+    for (int before = 0; base < tiles; base += 64) {
+      if (base) {
+        t = TreeTile{};
+        if (base + lane < tiles) t = tile_at(p, base + lane);
+      }
+      mine = pieces_of(t);
+      const int n = mine * p.c.heads, to = wave_scan(n);
+      here = __ballot(before + to > w);
+      if (here) {
+        at = __builtin_ctzll(here);
+        of = w - before - __builtin_amdgcn_readlane(to - n, at);
+        break;
+      }
+      before += __builtin_amdgcn_readlane(to, 63);
+    }
+    if (!here) return false;
+    out->slot = w;
+  }
+  out->t = {__builtin_amdgcn_readlane(t.b, at),      __builtin_amdgcn_readlane(t.q0, at),
+            __builtin_amdgcn_readlane(t.drafts, at), __builtin_amdgcn_readlane(t.rows, at),
+            __builtin_amdgcn_readlane(t.row0, at),   __builtin_amdgcn_readlane(t.past, at),
+            __builtin_amdgcn_readlane(t.lo, at),     __builtin_amdgcn_readlane(t.hi, at),
+            __builtin_amdgcn_readlane(t.steps, at)};
+  mine = __builtin_amdgcn_readlane(mine, at);
+  out->h = mine == 1 ? of : of / mine;
+  const int piece = of - out->h * mine, each = mine == 1 ? out->t.steps : (out->t.steps - 1) / mine + 1;
+  out->begin = piece * each;
+  out->end = min(out->t.steps, out->begin + each);
+  if (piece == 0 && threadIdx.x == 0)
+    info[static_cast<int64_t>(base + at) * p.c.heads + out->h] =
+        make_int4((out->t.steps - 1) / each + 1, out->slot, out->t.q0,
+                  out->t.row0 << 8 | min(p.tile_rows, out->t.rows - out->t.row0));
+  return out->begin < out->end;                      // (equal pieces may be fewer)
 }
 
-template <int D, typename TQ, int RG>
-__global__ __launch_bounds__(64 * kWaves) void tree_kernel(TreeParams p) {
-  __shared__ __attribute__((aligned(16))) TreeShared<D, RG, kWaves> sh;
+template <int D, typename TQ>
+__device__ __forceinline__ TQ* out_at(const TreeParams& p, int q0, int h, int row) {
+  const int query = p.by_group(row);
+  return static_cast<TQ*>(p.out) + (q0 + query) * p.ldo + static_cast<int64_t>(h * p.group + row - query * p.group) * D;
+}
+
+// The steps of a piece for RG groups of rows, and what comes of them: results, or a cut tile's sums.
+template <int D, typename TQ, int RG, int WAVES, int WIDE>
+__device__ __forceinline__ void take(const TreeParams& p, const Piece& me, int pages, Codes<D, WAVES>& codes,
+                                     bf16x8 (*queries)[64], uint32_t (*masks)[WIDE], int2* seers) {
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int index = blockIdx.x / p.c.heads, h = blockIdx.x - index * p.c.heads;
-  const int b = index / p.subs, sub = index - b * p.subs;
-  const TreeTile t = uniform(tree_tile(p, b, sub));
-  if (t.steps == 0) return;
-  load_masks<RG * kRowTile>(p, t, sh.mask);
+  const TreeTile& t = me.t;
   Sums<D> st[RG];
-  const int count = wave < t.steps ? (t.steps - wave + kWaves - 1) / kWaves : 0;
-  attend<D, TQ, RG, kWaves>(p, t, h, wave, count, look_up(p, b, t.lo, wave, kWaves), sh.mask, st);
+  const int first = me.begin + wave, count = first < me.end ? (me.end - first + WAVES - 1) / WAVES : 0;
+  attend<D, TQ, RG, WAVES, WIDE>(p, t, me.h, wave, first, count, pages, codes, queries, masks, seers, st);
+  // Each wave brings its sums to the maximum of all, and to their length where the result is whole; then
+  // they only have to be added.
+  const bool whole = me.end - me.begin == t.steps;
+  lds_barrier();                                     // the codes are read
+  if (g == 0)
+#pragma unroll
+    for (int r = 0; r < RG; ++r) codes.done.ml[wave][kRowTile * r + n] = make_float2(st[r].m, st[r].l);
+  lds_barrier();
+  float M[RG], L[RG];
 #pragma unroll
   for (int r = 0; r < RG; ++r) {
-    if (r) __syncthreads();
+    float2 ml[WAVES];
+    M[r] = kNoMax;
+    L[r] = 0.0f;
+#pragma unroll
+    for (int v = 0; v < WAVES; ++v) {
+      ml[v] = codes.done.ml[v][kRowTile * r + n];
+      M[r] = fmaxf(M[r], ml[v].x);
+    }
+#pragma unroll
+    for (int v = 0; v < WAVES; ++v) L[r] += __builtin_amdgcn_exp2f(ml[v].x - M[r]) * ml[v].y;
+    const float by = __builtin_amdgcn_exp2f(st[r].m - M[r]) * (!whole ? 1.0f : L[r] == 0.0f ? 0.0f : 1.0f / L[r]);
 #pragma unroll
     for (int c = 0; c < Sums<D>::NC; ++c)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float f[Sums<D>::NB];
+      for (int e = 0; e < Sums<D>::NB; ++e) st[r].o[c][e] *= by;
+    if (!whole && wave == 0 && g == 0 && t.row0 + kRowTile * r + n < t.rows)
+      *reinterpret_cast<float2*>(p.part_ml + 2 * (static_cast<int64_t>(me.slot) * p.tile_rows + kRowTile * r + n)) = make_float2(M[r], L[r]);
+  }
+#pragma unroll 1
+  for (int r = 0; r < RG; ++r) {
+    if (r) lds_barrier();                            // the last sums are read
 #pragma unroll
-        for (int e = 0; e < Sums<D>::NB; ++e) f[e] = st[r].o[c][e][i];
-        store_out<Sums<D>::NB>(sh.sums[wave][n] + Sums<D>::element(g, c, i), f);
-      }
-    if (g == 0) sh.ml[wave][n] = make_float2(st[r].m, st[r].l);
-    __syncthreads();
+    for (int x = 0; x < RG; ++x) {
+      if (x != r) continue;
+#pragma unroll
+      for (int c = 0; c < Sums<D>::NC; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float f[Sums<D>::NB];
+#pragma unroll
+          for (int e = 0; e < Sums<D>::NB; ++e) f[e] = st[x].o[c][e][i];
+          store_out<Sums<D>::NB>(codes.done.sums[wave][n] + Sums<D>::element(g, c, i), f);
+        }
+    }
+    lds_barrier();
     const int row0 = t.row0 + kRowTile * r;
-    for (int k = threadIdx.x; k < min(kRowTile, t.rows - row0) * (D / 8); k += 64 * kWaves) {
+    for (int k = threadIdx.x; k < min(kRowTile, t.rows - row0) * (D / 8); k += 64 * WAVES) {
       const int at = k / (D / 8), e = (k % (D / 8)) * 8;
-      float f[8];
-      const float L = join_waves<D, RG, kWaves>(sh, at, e, f).y;
-      const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+      float f[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+      constexpr int kWave = sizeof(codes.done.sums[0]);
+      const uint32_t from = lds_at(&codes.done.sums[0][at][e]);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) f[i] *= inv;
-      const int row = row0 + at, query = row / p.group;
-      store_out<8>(static_cast<TQ*>(p.out) + (t.q0 + query) * p.ldo +
-                       static_cast<int64_t>(h * p.group + row - query * p.group) * D + e, f);
+      for (int v = 0; v < WAVES; v += 4) add_four<kWave>(from + v * kWave, f);
+      if (whole) store_out<8>(out_at<D, TQ>(p, t.q0, me.h, row0 + at) + e, f);
+      else store_out<8>(p.part + (static_cast<int64_t>(me.slot) * p.tile_rows + kRowTile * r + at) * D + e, f);
     }
   }
 }
 
+// Waves of a workgroup: eight where there are few, four, of which a compute unit takes more, where there are
+// many; shared memory holds the codes of eight waves of heads of 256, and queries in 32 bits beside those of four.
+constexpr int waves_in(int d, int bytes, bool few) { return d == 256 ? (bytes == 4 ? 4 : 8) : few ? 8 : 4; }
+// Waves of a SIMD that the registers are for.
+constexpr int waves_of(int d, int bytes, int rg) {
+  return d == 256 ? (bytes == 4 ? 1 : 2) : bytes == 4 ? 2 : rg == 1 ? 4 : rg == 2 ? 3 : 2;
+}
+
+template <int D, typename TQ, int RG, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, waves_of(D, sizeof(TQ), RG)) void tree_kernel(TreeParams p) {
+  constexpr int kWide = Query<D, TQ, RG>::kMask;
+  __shared__ __attribute__((aligned(16))) Codes<D, WAVES> codes;
+  __shared__ __attribute__((aligned(16))) bf16x8 queries[Query<D, TQ, RG>::kShared ? Query<D, TQ, RG>::N : 1][64];
+  __shared__ uint32_t masks[RG * kRowTile][kWide];
+  __shared__ int2 seers[RG * kRowTile];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = blockIdx.x;
+  Piece me;
+  int pages = 0;
+  if (p.cut) {
+    if (!find_piece(p, w, &me)) return;
+    pages = look_up(p, me.t.b, me.t.lo, me.begin + wave, WAVES);
+  } else {
+    const int index = w / p.c.heads, b = p.subs == 1 ? index : index / p.subs;
+    // the first pages are on their way while the tile's length is
+    if (!p.window) pages = look_up(p, b, 0, wave, WAVES);
+    me.h = w - index * p.c.heads;
+    me.t = uniform(tree_tile(p, b, index - b * p.subs));
+    if (me.t.steps == 0) return;
+    if (p.window) pages = look_up(p, b, me.t.lo, wave, WAVES);
+    me.begin = me.slot = 0;
+    me.end = me.t.steps;
+  }
+  // (groups of rows that the tile does not have are left out)
+  const int rows = me.t.rows - me.t.row0;
+  if (RG == 1 || rows <= kRowTile) {
+    take<D, TQ, 1, WAVES, kWide>(p, me, pages, codes, queries, masks, seers);
+  } else if constexpr (RG >= 2) {
+    if (RG == 2 || rows <= 2 * kRowTile) {
+      take<D, TQ, 2, WAVES, kWide>(p, me, pages, codes, queries, masks, seers);
+    } else if constexpr (RG == 4) {
+      if (rows <= 3 * kRowTile) take<D, TQ, 3, WAVES, kWide>(p, me, pages, codes, queries, masks, seers);
+      else take<D, TQ, 4, WAVES, kWide>(p, me, pages, codes, queries, masks, seers);
+    }
+  }
+}
+
+// Joins the pieces of tile blockIdx.x (tile x head) for kJoinRows rows, in their order: a row's
+// threads take eight elements of every kGroups-th piece.
+constexpr int kJoinRows = 4;
+template <int D, typename TQ>
+__global__ __launch_bounds__(kJoinThreads) void tree_join_kernel(TreeParams p) {
+  constexpr int kPer = D / 8, kGroups = kJoinThreads / (kJoinRows * kPer);
+  __shared__ float4 part[kGroups][kJoinRows][kPer][2];
+  __shared__ float len[kGroups][kJoinRows];
+  const int4 info = reinterpret_cast<const int4*>(p.info)[blockIdx.x];
+  const int n = info.x, first = info.y;
+  auto row_of = [&](int k, int r) { return static_cast<int64_t>(first + k) * p.tile_rows + r; };
+  const int e = threadIdx.x % kPer, rr = threadIdx.x / kPer % kJoinRows, group = threadIdx.x / (kPer * kJoinRows);
+  const int r = blockIdx.y * kJoinRows + rr;
+  if (n < 2 || blockIdx.y * kJoinRows >= (info.w & 255)) return;
+  float L = 0.0f, f[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  if (r < (info.w & 255)) {
+    float M = kNoMax;
+#pragma unroll 4
+    for (int k = 0; k < n; ++k) M = fmaxf(M, p.part_ml[2 * row_of(k, r)]);
+#pragma unroll 4
+    for (int k = group; k < n; k += kGroups) {
+      const int64_t at = row_of(k, r);
+      const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + 2 * at);
+      const float4* o = reinterpret_cast<const float4*>(p.part + at * D + 8 * e);
+      const float4 x = o[0], y = o[1];
+      const float a = __builtin_amdgcn_exp2f(ml.x - M);
+      L += a * ml.y;
+      f[0] += a * x.x; f[1] += a * x.y; f[2] += a * x.z; f[3] += a * x.w;
+      f[4] += a * y.x; f[5] += a * y.y; f[6] += a * y.z; f[7] += a * y.w;
+    }
+  }
+  part[group][rr][e][0] = make_float4(f[0], f[1], f[2], f[3]);
+  part[group][rr][e][1] = make_float4(f[4], f[5], f[6], f[7]);
+  if (e == 0) len[group][rr] = L;
+  __syncthreads();
+  if (group != 0 || r >= (info.w & 255)) return;
+#pragma unroll
+  for (int k = 1; k < kGroups; ++k) {
+    L += len[k][rr];
+    const float4 x = part[k][rr][e][0], y = part[k][rr][e][1];
+    f[0] += x.x; f[1] += x.y; f[2] += x.z; f[3] += x.w;
+    f[4] += y.x; f[5] += y.y; f[6] += y.z; f[7] += y.w;
+  }
+  const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] *= inv;
+  store_out<8>(out_at<D, TQ>(p, info.z, blockIdx.x % p.c.heads, (info.w >> 8) + r) + 8 * e, f);
+}
+
+template <int D, typename TQ, int RG> void launch_tiles(const TreeParams& p, hipStream_t s) {
+  constexpr int kFew = waves_in(D, sizeof(TQ), true), kMany = waves_in(D, sizeof(TQ), false);
+  if (p.waves == kMany) tree_kernel<D, TQ, RG, kMany><<<p.groups, 64 * kMany, 0, s>>>(p);
+  else tree_kernel<D, TQ, RG, kFew><<<p.groups, 64 * kFew, 0, s>>>(p);
+  if (p.cut)
+    tree_join_kernel<D, TQ><<<dim3(static_cast<uint32_t>(p.B * p.subs * p.c.heads), p.tile_rows / kJoinRows), kJoinThreads, 0, s>>>(p);
+}
+
 template <int D, typename TQ> hipError_t launch(const TreeParams& p, hipStream_t s) {
-  const uint32_t groups = static_cast<uint32_t>(static_cast<int64_t>(p.B) * p.subs * p.c.heads);
-  tree_kernel<D, TQ, 1><<<groups, 64 * kWaves, 0, s>>>(p);
+  constexpr int kMost = most_groups(D, sizeof(TQ) == 4);
+  switch (p.tile_rows / kRowTile) {
+    case 1: launch_tiles<D, TQ, 1>(p, s); break;
+    case 2: if constexpr (kMost >= 2) launch_tiles<D, TQ, 2>(p, s); break;
+    default: if constexpr (kMost >= 4) launch_tiles<D, TQ, 4>(p, s); break;
+  }
   return hipGetLastError();
 }
 
 }  // namespace
 
 bool plan_tree(TreeParams* p, size_t* bytes) {
+  p->by_group = Divider(static_cast<uint32_t>(p->group));
   const int64_t rows = static_cast<int64_t>(p->max_q) * p->group;
-  p->tile_rows = kRowTile;
-  p->subs = static_cast<int>((rows + kRowTile - 1) / kRowTile);
-  *bytes = 16;
-  return static_cast<int64_t>(p->B) * p->subs * p->c.heads <= max_groups(64 * kWaves);
+  const int most = most_groups(p->c.d, p->dtype == CTS_F32);
+  int groups = 1;
+  while (groups < most && rows > groups * kRowTile) groups *= 2;
+  p->tile_rows = groups * kRowTile;
+  p->subs = static_cast<int>((rows + p->tile_rows - 1) / p->tile_rows);
+  const int64_t tiles = static_cast<int64_t>(p->B) * p->subs * p->c.heads;
+  int64_t span = p->max_kv;
+  if (p->window) span = std::min<int64_t>(span, static_cast<int64_t>(p->window) + p->max_q + kUnit);
+  const int64_t most_steps = std::max<int64_t>(1, (span + kUnit - 1) / kUnit);
+  if (tiles * 8 * most_steps > 0x50000000) return false;           // units are counted in 32 bits
+  const int bytes_of = p->dtype == CTS_F32 ? 4 : 2;
+  p->cut = most_steps > 32;
+  p->waves = waves_in(p->c.d, bytes_of, !p->cut && tiles < 256);
+  p->resident = 256 * std::max(1, 4 * waves_of(p->c.d, bytes_of, groups) / p->waves);
+  p->least = 8 * p->waves;                           // (two steps a wave)
+  // up to p->resident tiles are cut into that many pieces at most, more into half as many more than they are
+  int64_t pieces = std::max<int64_t>(p->resident, tiles + p->resident / 2);
+  pieces = !p->cut ? tiles : std::min(pieces, tiles * (6 * most_steps / p->least + 1));
+  if (pieces > max_groups(64 * kWaves) || tiles > max_groups(kJoinThreads)) return false;
+  p->groups = static_cast<uint32_t>(pieces);
+  const size_t slots = p->cut ? static_cast<size_t>(pieces) * p->tile_rows : 0;
+  *bytes = slots * (p->c.d + 2) * sizeof(float) + (p->cut ? static_cast<size_t>(tiles) * 16 : 0) + 16;
+  return true;
+}
+
+void place_tree(TreeParams* p, void* workspace) {
+  const size_t slots = static_cast<size_t>(p->groups) * p->tile_rows;
+  p->part = static_cast<float*>(workspace);
+  p->part_ml = p->part + slots * p->c.d;
+  p->info = reinterpret_cast<int32_t*>(p->part_ml + slots * 2);
 }
 
 hipError_t launch_tree(const TreeParams& p, hipStream_t s) {

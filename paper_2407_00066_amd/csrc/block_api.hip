@@ -316,6 +316,7 @@ int cts_kv_tree_attention(const cts_attn_problem* p, const cts_kv_cache* c, cons
   if (meets(extent(rows(out, p->T, width, ldo, p->dtype)), more, 2) || meets(r[7], more, 2)) return CTS_ERR_INVALID_ARG;
   if (workspace_bytes < need) return CTS_ERR_WORKSPACE;
   a.mask = mask; a.mask_words = mask_words; a.positions = positions;
+  cts::place_tree(&a, workspace);
   return status(cts::launch_tree(a, static_cast<hipStream_t>(stream)));
 }
 

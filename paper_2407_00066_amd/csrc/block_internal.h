@@ -90,8 +90,15 @@ struct TreeParams : AttnParams {
   const uint32_t* mask; int64_t mask_words;     // [T][mask_words]
   const int32_t* positions;                     // of the rows, with a window
   int tile_rows;
+  Divider by_group;
+  // whether tiles are cut along their tokens; workgroups; how many run at a time; units of work of a
+  // piece at least; waves of a workgroup
+  bool cut;
+  uint32_t groups;
+  int resident, least, waves;
 };
 bool plan_tree(TreeParams* p, size_t* bytes);
+void place_tree(TreeParams* p, void* workspace);
 hipError_t launch_tree(const TreeParams& p, hipStream_t s);
 
 struct NormParams {
