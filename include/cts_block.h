@@ -191,6 +191,12 @@ int cts_kv_append(const cts_kv_cache* c, int32_t T, int32_t n_q_heads, int32_t r
  * max_q are left out as rows, and as drafts that others see. */
 size_t cts_kv_tree_attention_workspace_size(const cts_attn_problem* p, const cts_kv_cache* c);
 
+/* How a call with these sizes takes its work, for tests and debugging; plan is a host
+ * array of 3 entries: [0] query rows (row x head of a key/value head's group) that share a
+ * walk over the tokens, at most; [1] 0: a workgroup takes all of a tile's tokens, 1: the same,
+ * tiles with most work first, 2: tiles are cut along their tokens; [2] waves of a workgroup. */
+int cts_kv_tree_attention_plan(const cts_attn_problem* p, const cts_kv_cache* c, int32_t* plan);
+
 int cts_kv_tree_attention(const cts_attn_problem* p, const cts_kv_cache* c, const void* q, int64_t ldq,
                           const int32_t* block_table, const int32_t* kv_len, const int32_t* q_start, const uint32_t* mask,
                           int64_t mask_words, const int32_t* positions, void* out, int64_t ldo, void* workspace,

@@ -10,4 +10,5 @@ from ._binding import (CtsError, Problem, apply, apply_diag, apply_multi, apply_
                        validate_ids, workspace_bucketing, workspace_size, workspace_size_multi,
                        CTS_F32, CTS_BF16, NOALLOC_SCRATCH_BYTES)
 from .block import (KVCache, block_norm, kv_append, kv_attention, kv_attention_plan, kv_attention_workspace_size,  # noqa: F401
-                    kv_cache, kv_keep, kv_read, kv_tree_attention, kv_tree_attention_workspace_size, kv_write, rotary)
+                    kv_cache, kv_keep, kv_read, kv_tree_attention, kv_tree_attention_plan, kv_tree_attention_workspace_size,
+                    kv_write, rotary)

@@ -66,8 +66,8 @@ EXPORTED = ("cts_status_string", "cts_workspace_size", "cts_workspace_size_uncom
             "cts_jd_diag", "cts_jd_sigma", "cts_jd_cluster",
             # include/cts_block.h
             "cts_kv_write", "cts_kv_read", "cts_kv_attention_workspace_size", "cts_kv_attention_plan", "cts_kv_attention",
-            "cts_block_norm", "cts_rotary", "cts_kv_append", "cts_kv_tree_attention_workspace_size", "cts_kv_tree_attention",
-            "cts_kv_keep")
+            "cts_block_norm", "cts_rotary", "cts_kv_append", "cts_kv_tree_attention_workspace_size", "cts_kv_tree_attention_plan",
+            "cts_kv_tree_attention", "cts_kv_keep")
 N_STAGE_EVENTS = 6
 
 
@@ -192,6 +192,8 @@ def lib() -> ctypes.CDLL:
                 L.cts_kv_append.restype = ctypes.c_int
                 L.cts_kv_tree_attention_workspace_size.argtypes = [ap, cp]
                 L.cts_kv_tree_attention_workspace_size.restype = sz
+                L.cts_kv_tree_attention_plan.argtypes = [ap, cp, ctypes.POINTER(i32)]
+                L.cts_kv_tree_attention_plan.restype = ctypes.c_int
                 L.cts_kv_tree_attention.argtypes = [ap, cp, vp, i64, vp, vp, vp, vp, i64, vp, vp, i64, vp, sz, vp]
                 L.cts_kv_tree_attention.restype = ctypes.c_int
                 L.cts_kv_keep.argtypes = [cp, i32, i32, vp, vp, vp, i32, vp, vp, vp]

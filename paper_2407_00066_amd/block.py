@@ -289,6 +289,16 @@ def kv_tree_attention_workspace_size(q, cache: KVCache, B, max_q, max_kv, window
     return int(lib().cts_kv_tree_attention_workspace_size(ctypes.byref(p), ctypes.byref(cache._c)))
 
 
+def kv_tree_attention_plan(q, cache: KVCache, block_table, max_q, max_kv, window=0) -> tuple:
+    """(rows, how, waves) of kv_tree_attention for tensors like these, for tests and
+    debugging: how in "whole", "by work", "cut" (see cts_kv_tree_attention_plan)."""
+    B, cols = block_table.shape
+    p = AttnProblem(q.shape[0], B, q.shape[1], cols, max_q, max_kv, window, _dt(q, "q"), 1.0)
+    out = (ctypes.c_int32 * 3)()
+    _check(lib().cts_kv_tree_attention_plan(ctypes.byref(p), ctypes.byref(cache._c), out), "cts_kv_tree_attention_plan")
+    return out[0], ("whole", "by work", "cut")[out[1]], out[2]
+
+
 def kv_tree_attention(q, cache: KVCache, block_table, kv_len, mask, q_start=None, max_q=None, max_kv=None, scale=None,
                       window=0, positions=None, out=None, workspace=None):
     """Attention of drafted tokens q [T, n_q_heads, head_dim]: each sequence's rows

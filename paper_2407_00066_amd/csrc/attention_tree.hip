@@ -17,6 +17,8 @@
 namespace cts {
 namespace {
 
+constexpr int kMaskWords = kTreeMaxQ / 32 + 2;     // of a query, in shared memory
+
 struct TreeTile {
   int b, q0, drafts, rows, row0;   // the sequence, its first query row, the drafts that count, its rows, the tile's first
   int past;                        // position of the first draft
@@ -49,6 +51,9 @@ __device__ __forceinline__ TreeTile uniform(TreeTile t) {
           __builtin_amdgcn_readfirstlane(t.steps)};
 }
 
+// Kinds of instructions to the scheduler.
+constexpr int kValu = 0x2, kMatrix = 0x8, kLdsRead = 0x100;
+
 // The maximum of a row that has seen nothing: finite, so that no step asks whether there is one.
 constexpr float kNoMax = -3.0e38f;
 
@@ -72,8 +77,6 @@ constexpr int most_groups(int d, bool f32) { return d == 256 ? (f32 ? 1 : 2) : f
 template <int D, typename TQ, int RG> struct Query {
   static constexpr int NS = sizeof(TQ) == 4 ? 3 : 1, KS = D / 32, N = RG * KS * NS;
   static constexpr bool kShared = N > 6;
-  // words of a query's mask: a tile of fewer rows than the most has all of its sequence's
-  static constexpr int kMask = 2 + (RG == most_groups(D, sizeof(TQ) == 4) ? kTreeMaxQ / 32 : 1);
 };
 
 // A step's codes and scales, loaded straight into shared memory where the lane that loads
@@ -113,6 +116,9 @@ __device__ __forceinline__ void load_lds4(const uint8_t* at, char* lds) {
                                    (__attribute__((address_space(3))) void*)lds, 4, 0, 0);
 #endif
 }
+
+// The bytes of w that are past 252, as their highest bits.
+__device__ __forceinline__ uint32_t over_252(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x03030303u) & w & 0x80808080u; }
 
 // A step's keys and their scales of both groups of 16 tokens, from shared memory: reads and their wait in
 // one piece of assembly (as plain reads they would wait for the next step's loads too).
@@ -217,9 +223,9 @@ template <int STRIDE> __device__ __forceinline__ void add_four(uint32_t at, floa
 
 // `count` of the tile's steps from s0, `stride` apart, for key/value head h, by
 // wave `wave`; pages: look_up of the first 32.  The workgroup meets once, for masks and queries.
-template <int D, typename TQ, int RG, int stride, int WIDE>
+template <int D, typename TQ, int RG, int stride>
 __device__ __forceinline__ void attend(const TreeParams& p, const TreeTile& t, int h, int wave, int s0, int count, int pages,
-                                       Codes<D, stride>& codes, bf16x8 (*queries)[64], uint32_t (*masks)[WIDE], int2* seers, Sums<D>* st) {
+                                       Codes<D, stride>& codes, bf16x8 (*queries)[64], uint32_t (*masks)[kMaskWords], int2* seers, Sums<D>* st) {
   using Q = Query<D, TQ, RG>;
   using S = Step<D>;
   constexpr int NS = Q::NS, KS = Q::KS;          // (KS: steps of the first product; words of keys a lane holds)
@@ -296,9 +302,9 @@ __device__ __forceinline__ void attend(const TreeParams& p, const TreeTile& t, i
   };
   // All that is needed is asked for before any of it is waited for: the masks' first words, the queries, then the codes.
   const int q_first = p.by_group(t.row0), q_last = p.by_group(min(t.rows, t.row0 + RG * kRowTile) - 1);
-  const int words = (q_last - q_first + 1) * WIDE;
+  const int words = (q_last - q_first + 1) * kMaskWords;
   uint32_t word = 0;
-  if (static_cast<int>(threadIdx.x) < words) word = mask_word(p, t, q_first, threadIdx.x / WIDE, static_cast<int>(threadIdx.x % WIDE) - 1);
+  if (static_cast<int>(threadIdx.x) < words) word = mask_word(p, t, q_first, threadIdx.x / kMaskWords, static_cast<int>(threadIdx.x % kMaskWords) - 1);
   bf16x8 qf[Q::kShared ? 1 : RG][KS][NS];
   auto query_at = [&](int r, bool* live) -> const TQ* {
     const int row = t.row0 + kRowTile * r + n, query = p.by_group(row);
@@ -328,8 +334,8 @@ __device__ __forceinline__ void attend(const TreeParams& p, const TreeTile& t, i
 #pragma unroll
     for (int i = 0; i < S::kSlots - 1; ++i) ask(min(i, count - 1));
   for (int k = threadIdx.x; k < words; k += 64 * stride) {
-    if (k >= 64 * stride) word = mask_word(p, t, q_first, k / WIDE, k % WIDE - 1);
-    masks[k / WIDE][k % WIDE] = word;
+    if (k >= 64 * stride) word = mask_word(p, t, q_first, k / kMaskWords, k % kMaskWords - 1);
+    masks[k / kMaskWords][k % kMaskWords] = word;
   }
   if (threadIdx.x < RG * kRowTile) seers[threadIdx.x] = seer;           // (the first wave's)
 #pragma unroll
@@ -382,6 +388,10 @@ __device__ __forceinline__ void attend(const TreeParams& p, const TreeTile& t, i
     f32x4 x[RG][2];
     {
       uint32_t k[2][KS], ks[2];
+      bf16x8 b[2][Q::kShared ? RG * NS : 1];         // the rows' pieces that are multiplied, and the next ones
+      if constexpr (Q::kShared)
+#pragma unroll
+        for (int e = 0; e < RG * NS; ++e) b[0][e] = queries[(e / NS * KS) * NS + e % NS][lane];
       read_keys<D>(from, lane, k, ks);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
@@ -391,6 +401,10 @@ __device__ __forceinline__ void attend(const TreeParams& p, const TreeTile& t, i
       }
 #pragma unroll
       for (int y = 0; y < KS; ++y) {
+        if constexpr (Q::kShared)
+          if (y + 1 < KS)
+#pragma unroll
+            for (int e = 0; e < RG * NS; ++e) b[(y + 1) & 1][e] = queries[(e / NS * KS + y + 1) * NS + e % NS][lane];
         bf16x8 a[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -400,11 +414,22 @@ __device__ __forceinline__ void attend(const TreeParams& p, const TreeTile& t, i
 #pragma unroll
         for (int r = 0; r < RG; ++r)
 #pragma unroll
-          for (int z = 0; z < NS; ++z) {
-            const bf16x8 b = Q::kShared ? queries[Q::kShared ? (r * KS + y) * NS + z : 0][lane] : qf[Q::kShared ? 0 : r][y][z];
+          for (int z = 0; z < NS; ++z)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) x[r][i] = mfma(a[i], b, x[r][i]);
+            for (int i = 0; i < 2; ++i) x[r][i] = mfma(a[i], Q::kShared ? b[y & 1][Q::kShared ? r * NS + z : 0] : qf[Q::kShared ? 0 : r][y][z], x[r][i]);
+      }
+      // The next keys are converted behind the products of these.
+      if constexpr (RG >= 2) {
+        __builtin_amdgcn_sched_group_barrier(kValu, 10, 0);
+#pragma unroll
+        for (int y = 0; y < KS; ++y) {
+          if (Q::kShared && y + 1 < KS) __builtin_amdgcn_sched_group_barrier(kLdsRead, RG * NS, 0);
+#pragma unroll
+          for (int j = 0; j < 2 * RG * NS; ++j) {
+            __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(kValu, RG * NS >= 4 ? 1 : 2, 0);
           }
+        }
       }
     }
     uint32_t v[2][NC][4], vs[2][NC];
@@ -433,8 +458,10 @@ __device__ __forceinline__ void attend(const TreeParams& p, const TreeTile& t, i
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (!(bits >> (16 * i + j) & 1)) x[r][i][j] = -INFINITY;
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t keep = static_cast<uint32_t>(static_cast<int32_t>(bits << (31 - 16 * i - j)) >> 31);
+            x[r][i][j] = __uint_as_float((__float_as_uint(x[r][i][j]) & keep) | (0xff800000u & ~keep));
+          }
       }
     }
     // The maxima are looked at lane by lane, and across lanes only where one has grown past the slack.
@@ -484,13 +511,13 @@ __device__ __forceinline__ void attend(const TreeParams& p, const TreeTile& t, i
       if (masked) {
         // A weight of zero does not hide a NaN or infinite value: blocks that can hold one are
         // taken out of the product, and the rows that do see one are made NaN.
-        uint32_t hit[4] = {0, 0, 0, 0};
+        if (__any((over_252(vs[0][c]) | over_252(vs[1][c])) != 0)) {
+          uint32_t hit[4] = {0, 0, 0, 0};
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+          for (int i = 0; i < 2; ++i)
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (past_scales(rare(static_cast<int>(vs[i][c])), j)) hit[2 * i + j / 2] |= 0x3f80u << (16 * (j & 1));
-        if (__any((hit[0] | hit[1] | hit[2] | hit[3]) != 0)) {
+            for (int j = 0; j < 4; ++j)
+              if (past_scales(vs[i][c], j)) hit[2 * i + j / 2] |= 0x3f80u << (16 * (j & 1));
 #pragma unroll
           for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -538,6 +565,15 @@ __device__ __forceinline__ void attend(const TreeParams& p, const TreeTile& t, i
             st[r].o[c][2 * e + 1] = mfma(odd, pf[r][z], st[r].o[c][2 * e + 1]);
           }
       }
+      // (the same of values: 24 instructions for 2 RG products)
+      if constexpr (RG >= 2) {
+        __builtin_amdgcn_sched_group_barrier(kValu, 28, 0);
+#pragma unroll
+        for (int j = 0; j < NB * RG * NS; ++j) {
+          __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(kValu, RG * NS >= 4 ? 3 : RG * NS == 3 ? 4 : 6, 0);
+        }
+      }
     }
   }
 #pragma unroll
@@ -561,11 +597,14 @@ __device__ __forceinline__ TreeTile tile_at(const TreeParams& p, int i) {
   return tree_tile(p, b, i - b * p.subs);
 }
 
-// Piece w of the batch; false: there are not so many.  As long as there are no more tiles than workgroups that run
-// at a time, they are cut along their tokens into equal pieces until there are as many of those; of more tiles,
-// those whose work is past twice a workgroup's share of all.  Up to 64 tiles (of a head) are taken by the length
-// of their pieces, to an eighth: the longest first, one to a compute unit, then the shortest beside
-// them, then the others as workgroups end.
+// What comes before and after a piece's steps, in units.
+constexpr int kAround = 100;
+
+// Piece w of the batch; false: there are not so many.  Tiles are cut along their tokens into equal pieces.  With
+// few tiles there are no more pieces than workgroups that run at a time, since a second round would take as
+// long as the first; otherwise a piece is at most a workgroup's share of the work, and what more pieces
+// would take.  Up to 64 tiles (of a head) are taken by the length of their pieces, to an eighth: the
+// longest first, one to a compute unit, then the shortest beside them, then the others as workgroups end.
 __device__ __forceinline__ bool find_piece(const TreeParams& p, int w, Piece* out) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tiles = p.B * p.subs;
   int4* const info = reinterpret_cast<int4*>(p.info);
@@ -584,8 +623,11 @@ __device__ __forceinline__ bool find_piece(const TreeParams& p, int w, Piece* ou
   total *= p.c.heads;
   some *= p.c.heads;
   if (total == 0) return false;
-  const bool few = some <= p.resident && tiles <= 64;
-  int len = max(p.least, (few ? 1 : 2) * ((total - 1) / p.resident + 1));
+  const bool few = some <= (tiles <= 64 ? p.resident : p.resident / 2);
+  int len;
+  if (few) len = (total - 1) / (p.resident - (tiles <= 64 ? some / 2 : some)) + 1;
+  else len = total / p.resident + total / p.resident / 8 + some * (kAround * 5 / 8) / p.resident;
+  len = max(len, p.least);
   auto pieces_of = [&](const TreeTile& t) {
     const int units = t.steps * unit_of(t, p.tile_rows);
     return units <= len ? (units > 0 ? 1 : 0) : static_cast<int>(static_cast<float>(units) * __builtin_amdgcn_rcpf(static_cast<float>(len))) + 1;
@@ -594,7 +636,7 @@ __device__ __forceinline__ bool find_piece(const TreeParams& p, int w, Piece* ou
   TreeTile t = t0;
   if (tiles <= 64) {
     int n;
-    for (;; len += len / 16 + 1) {
+    for (;; len += len / 8) {
       mine = pieces_of(t);
       n = __builtin_amdgcn_readlane(wave_scan(mine), 63) * p.c.heads;
       if (!few || n <= p.resident) break;
@@ -641,7 +683,9 @@ __device__ __forceinline__ bool find_piece(const TreeParams& p, int w, Piece* ou
             __builtin_amdgcn_readlane(t.steps, at)};
   mine = __builtin_amdgcn_readlane(mine, at);
   out->h = mine == 1 ? of : of / mine;
-  const int piece = of - out->h * mine, each = mine == 1 ? out->t.steps : (out->t.steps - 1) / mine + 1;
+  // (a multiple of its waves' number: they end together)
+  const int piece = of - out->h * mine;
+  const int each = mine == 1 ? out->t.steps : ((out->t.steps - 1) / mine + p.waves) & -p.waves;
   out->begin = piece * each;
   out->end = min(out->t.steps, out->begin + each);
   if (piece == 0 && threadIdx.x == 0)
@@ -651,6 +695,37 @@ __device__ __forceinline__ bool find_piece(const TreeParams& p, int w, Piece* ou
   return out->begin < out->end;                      // (equal pieces may be fewer)
 }
 
+// The tile (of a head) whose work is the rank-th most, to an eighth of the most there can be; of up to kOrdered tiles.
+// With more workgroups than compute units the longest go first: they would end last.
+constexpr int kOrdered = 256;
+__device__ __forceinline__ int tile_of_rank(const TreeParams& p, int rank) {
+  constexpr int kEach = kOrdered / 64;
+  const int lane = threadIdx.x & 63, tiles = p.B * p.subs;
+  const float scale = 8.0f / static_cast<float>(p.most_units);
+  int bucket[kEach];
+#pragma unroll
+  for (int c = 0; c < kEach; ++c) {
+    const int i = 64 * c + lane;
+    bucket[c] = -1;
+    if (i < tiles) {
+      const TreeTile t = tile_at(p, i);
+      bucket[c] = min(7, static_cast<int>(static_cast<float>(t.steps * unit_of(t, p.tile_rows)) * scale));
+    }
+  }
+  for (int k = 7; k >= 0; --k)
+#pragma unroll
+    for (int c = 0; c < kEach; ++c) {
+      const uint64_t here = __ballot(bucket[c] == k);
+      const int n = __builtin_popcountll(here);
+      if (rank < n) {
+        const int below = __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(here >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(here), 0));
+        return 64 * c + __builtin_ctzll(__ballot(bucket[c] == k && below == rank));
+      }
+      rank -= n;
+    }
+  return 0;                                          // (every tile is in a bucket)
+}
+
 template <int D, typename TQ>
 __device__ __forceinline__ TQ* out_at(const TreeParams& p, int q0, int h, int row) {
   const int query = p.by_group(row);
@@ -658,15 +733,15 @@ __device__ __forceinline__ TQ* out_at(const TreeParams& p, int q0, int h, int ro
 }
 
 // The steps of a piece for RG groups of rows, and what comes of them: results, or a cut tile's sums.
-template <int D, typename TQ, int RG, int WAVES, int WIDE>
+template <int D, typename TQ, int RG, int WAVES>
 __device__ __forceinline__ void take(const TreeParams& p, const Piece& me, int pages, Codes<D, WAVES>& codes,
-                                     bf16x8 (*queries)[64], uint32_t (*masks)[WIDE], int2* seers) {
+                                     bf16x8 (*queries)[64], uint32_t (*masks)[kMaskWords], int2* seers) {
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const TreeTile& t = me.t;
   Sums<D> st[RG];
   const int first = me.begin + wave, count = first < me.end ? (me.end - first + WAVES - 1) / WAVES : 0;
-  attend<D, TQ, RG, WAVES, WIDE>(p, t, me.h, wave, first, count, pages, codes, queries, masks, seers, st);
+  attend<D, TQ, RG, WAVES>(p, t, me.h, wave, first, count, pages, codes, queries, masks, seers, st);
   // Each wave brings its sums to the maximum of all, and to their length where the result is whole; then
   // they only have to be added.
   const bool whole = me.end - me.begin == t.steps;
@@ -737,10 +812,9 @@ constexpr int waves_of(int d, int bytes, int rg) {
 
 template <int D, typename TQ, int RG, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, waves_of(D, sizeof(TQ), RG)) void tree_kernel(TreeParams p) {
-  constexpr int kWide = Query<D, TQ, RG>::kMask;
   __shared__ __attribute__((aligned(16))) Codes<D, WAVES> codes;
   __shared__ __attribute__((aligned(16))) bf16x8 queries[Query<D, TQ, RG>::kShared ? Query<D, TQ, RG>::N : 1][64];
-  __shared__ uint32_t masks[RG * kRowTile][kWide];
+  __shared__ uint32_t masks[RG * kRowTile][kMaskWords];
   __shared__ int2 seers[RG * kRowTile];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = blockIdx.x;
   Piece me;
@@ -749,10 +823,12 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(D, sizeof(TQ), RG)) void tree_
     if (!find_piece(p, w, &me)) return;
     pages = look_up(p, me.t.b, me.t.lo, me.begin + wave, WAVES);
   } else {
-    const int index = w / p.c.heads, b = p.subs == 1 ? index : index / p.subs;
-    // the first pages are on their way while the tile's length is
-    if (!p.window) pages = look_up(p, b, 0, wave, WAVES);
+    int index = w / p.c.heads;
     me.h = w - index * p.c.heads;
+    // the first pages are on their way while the tile's length is
+    if (p.ordered) index = tile_of_rank(p, index);
+    const int b = p.subs == 1 ? index : index / p.subs;
+    if (!p.window) pages = look_up(p, b, 0, wave, WAVES);
     me.t = uniform(tree_tile(p, b, index - b * p.subs));
     if (me.t.steps == 0) return;
     if (p.window) pages = look_up(p, b, me.t.lo, wave, WAVES);
@@ -762,73 +838,80 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(D, sizeof(TQ), RG)) void tree_
   // (groups of rows that the tile does not have are left out)
   const int rows = me.t.rows - me.t.row0;
   if (RG == 1 || rows <= kRowTile) {
-    take<D, TQ, 1, WAVES, kWide>(p, me, pages, codes, queries, masks, seers);
+    take<D, TQ, 1, WAVES>(p, me, pages, codes, queries, masks, seers);
   } else if constexpr (RG >= 2) {
     if (RG == 2 || rows <= 2 * kRowTile) {
-      take<D, TQ, 2, WAVES, kWide>(p, me, pages, codes, queries, masks, seers);
+      take<D, TQ, 2, WAVES>(p, me, pages, codes, queries, masks, seers);
     } else if constexpr (RG == 4) {
-      if (rows <= 3 * kRowTile) take<D, TQ, 3, WAVES, kWide>(p, me, pages, codes, queries, masks, seers);
-      else take<D, TQ, 4, WAVES, kWide>(p, me, pages, codes, queries, masks, seers);
+      if (rows <= 3 * kRowTile) take<D, TQ, 3, WAVES>(p, me, pages, codes, queries, masks, seers);
+      else take<D, TQ, 4, WAVES>(p, me, pages, codes, queries, masks, seers);
     }
   }
 }
 
-// Joins the pieces of tile blockIdx.x (tile x head) for kJoinRows rows, in their order: a row's
+// Joins the pieces of tile blockIdx.x (tile x head) for join_rows rows, in their order: kRows rows at a time, whose
 // threads take eight elements of every kGroups-th piece.
-constexpr int kJoinRows = 4;
 template <int D, typename TQ>
 __global__ __launch_bounds__(kJoinThreads) void tree_join_kernel(TreeParams p) {
-  constexpr int kPer = D / 8, kGroups = kJoinThreads / (kJoinRows * kPer);
-  __shared__ float4 part[kGroups][kJoinRows][kPer][2];
-  __shared__ float len[kGroups][kJoinRows];
+  constexpr int kPer = D / 8, kRows = 4, kGroups = kJoinThreads / (kRows * kPer);
+  __shared__ float4 part[kGroups][kRows][kPer][2];
+  __shared__ float len[kGroups][kRows];
   const int4 info = reinterpret_cast<const int4*>(p.info)[blockIdx.x];
-  const int n = info.x, first = info.y;
-  auto row_of = [&](int k, int r) { return static_cast<int64_t>(first + k) * p.tile_rows + r; };
-  const int e = threadIdx.x % kPer, rr = threadIdx.x / kPer % kJoinRows, group = threadIdx.x / (kPer * kJoinRows);
-  const int r = blockIdx.y * kJoinRows + rr;
-  if (n < 2 || blockIdx.y * kJoinRows >= (info.w & 255)) return;
-  float L = 0.0f, f[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-  if (r < (info.w & 255)) {
-    float M = kNoMax;
+  const int n = info.x, rows = info.w & 255;
+  if (n < 2) return;
+  auto row_of = [&](int k, int r) { return static_cast<int64_t>(info.y + k) * p.tile_rows + r; };
+  const int e = threadIdx.x % kPer, rr = threadIdx.x / kPer % kRows, group = threadIdx.x / (kPer * kRows);
+  for (int r0 = blockIdx.y * p.join_rows; r0 < min(rows, static_cast<int>(blockIdx.y + 1) * p.join_rows); r0 += kRows) {
+    const int r = r0 + rr;
+    float L = 0.0f, f[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (r < rows) {
+      float M = kNoMax;                              // (the row's threads look at a piece each)
+      for (int k = e; k < n; k += kPer) M = fmaxf(M, p.part_ml[2 * row_of(k, r)]);
+#pragma unroll
+      for (int x = 1; x < kPer; x <<= 1) M = fmaxf(M, __shfl_xor(M, x));
 #pragma unroll 4
-    for (int k = 0; k < n; ++k) M = fmaxf(M, p.part_ml[2 * row_of(k, r)]);
-#pragma unroll 4
-    for (int k = group; k < n; k += kGroups) {
-      const int64_t at = row_of(k, r);
-      const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + 2 * at);
-      const float4* o = reinterpret_cast<const float4*>(p.part + at * D + 8 * e);
-      const float4 x = o[0], y = o[1];
-      const float a = __builtin_amdgcn_exp2f(ml.x - M);
-      L += a * ml.y;
-      f[0] += a * x.x; f[1] += a * x.y; f[2] += a * x.z; f[3] += a * x.w;
-      f[4] += a * y.x; f[5] += a * y.y; f[6] += a * y.z; f[7] += a * y.w;
+      for (int k = group; k < n; k += kGroups) {
+        const int64_t at = row_of(k, r);
+        const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + 2 * at);
+        const float4* o = reinterpret_cast<const float4*>(p.part + at * D + 8 * e);
+        const float4 x = o[0], y = o[1];
+        const float a = __builtin_amdgcn_exp2f(ml.x - M);
+        L += a * ml.y;
+        f[0] += a * x.x; f[1] += a * x.y; f[2] += a * x.z; f[3] += a * x.w;
+        f[4] += a * y.x; f[5] += a * y.y; f[6] += a * y.z; f[7] += a * y.w;
+      }
     }
-  }
-  part[group][rr][e][0] = make_float4(f[0], f[1], f[2], f[3]);
-  part[group][rr][e][1] = make_float4(f[4], f[5], f[6], f[7]);
-  if (e == 0) len[group][rr] = L;
-  __syncthreads();
-  if (group != 0 || r >= (info.w & 255)) return;
+    part[group][rr][e][0] = make_float4(f[0], f[1], f[2], f[3]);
+    part[group][rr][e][1] = make_float4(f[4], f[5], f[6], f[7]);
+    if (e == 0) len[group][rr] = L;
+    lds_barrier();
+    if (group == 0 && r < rows) {
 #pragma unroll
-  for (int k = 1; k < kGroups; ++k) {
-    L += len[k][rr];
-    const float4 x = part[k][rr][e][0], y = part[k][rr][e][1];
-    f[0] += x.x; f[1] += x.y; f[2] += x.z; f[3] += x.w;
-    f[4] += y.x; f[5] += y.y; f[6] += y.z; f[7] += y.w;
-  }
-  const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+      for (int k = 1; k < kGroups; ++k) {
+        L += len[k][rr];
+        const float4 x = part[k][rr][e][0], y = part[k][rr][e][1];
+        f[0] += x.x; f[1] += x.y; f[2] += x.z; f[3] += x.w;
+        f[4] += y.x; f[5] += y.y; f[6] += y.z; f[7] += y.w;
+      }
+      const float inv = L == 0.0f ? 0.0f : 1.0f / L;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) f[i] *= inv;
-  store_out<8>(out_at<D, TQ>(p, info.z, blockIdx.x % p.c.heads, (info.w >> 8) + r) + 8 * e, f);
+      for (int i = 0; i < 8; ++i) f[i] *= inv;
+      store_out<8>(out_at<D, TQ>(p, info.z, blockIdx.x % p.c.heads, (info.w >> 8) + r) + 8 * e, f);
+    }
+    lds_barrier();
+  }
 }
 
 template <int D, typename TQ, int RG> void launch_tiles(const TreeParams& p, hipStream_t s) {
   constexpr int kFew = waves_in(D, sizeof(TQ), true), kMany = waves_in(D, sizeof(TQ), false);
-  if (p.waves == kMany) tree_kernel<D, TQ, RG, kMany><<<p.groups, 64 * kMany, 0, s>>>(p);
-  else tree_kernel<D, TQ, RG, kFew><<<p.groups, 64 * kFew, 0, s>>>(p);
+  if (p.waves == kMany) tree_kernel<D, TQ, RG, kMany><<<static_cast<uint32_t>(p.groups), 64 * kMany, 0, s>>>(p);
+  else tree_kernel<D, TQ, RG, kFew><<<static_cast<uint32_t>(p.groups), 64 * kFew, 0, s>>>(p);
   if (p.cut)
-    tree_join_kernel<D, TQ><<<dim3(static_cast<uint32_t>(p.B * p.subs * p.c.heads), p.tile_rows / kJoinRows), kJoinThreads, 0, s>>>(p);
+    tree_join_kernel<D, TQ><<<dim3(static_cast<uint32_t>(p.B * p.subs * p.c.heads), p.tile_rows / p.join_rows), kJoinThreads, 0, s>>>(p);
 }
+
+// Steps of all tiles up to which tiles of fewer rows are taken.
+constexpr int64_t kLittleWork = 8192;
 
 template <int D, typename TQ> hipError_t launch(const TreeParams& p, hipStream_t s) {
   constexpr int kMost = most_groups(D, sizeof(TQ) == 4);
@@ -842,31 +925,50 @@ template <int D, typename TQ> hipError_t launch(const TreeParams& p, hipStream_t
 
 }  // namespace
 
-bool plan_tree(TreeParams* p, size_t* bytes) {
-  p->by_group = Divider(static_cast<uint32_t>(p->group));
+// The plan for tiles of `groups` groups of rows over `steps` steps at most; the workspace's bytes.
+static size_t plan_groups(TreeParams* p, int groups, int64_t steps) {
+  const int bytes_of = p->dtype == CTS_F32 ? 4 : 2;
   const int64_t rows = static_cast<int64_t>(p->max_q) * p->group;
-  const int most = most_groups(p->c.d, p->dtype == CTS_F32);
-  int groups = 1;
-  while (groups < most && rows > groups * kRowTile) groups *= 2;
   p->tile_rows = groups * kRowTile;
   p->subs = static_cast<int>((rows + p->tile_rows - 1) / p->tile_rows);
   const int64_t tiles = static_cast<int64_t>(p->B) * p->subs * p->c.heads;
-  int64_t span = p->max_kv;
-  if (p->window) span = std::min<int64_t>(span, static_cast<int64_t>(p->window) + p->max_q + kUnit);
-  const int64_t most_steps = std::max<int64_t>(1, (span + kUnit - 1) / kUnit);
-  if (tiles * 8 * most_steps > 0x50000000) return false;           // units are counted in 32 bits
-  const int bytes_of = p->dtype == CTS_F32 ? 4 : 2;
-  p->cut = most_steps > 32;
+  p->cut = steps > 64 && (tiles < 512 || steps > std::min<int64_t>(256, tiles / 4));
+  p->ordered = !p->cut && tiles > 256 && p->B * static_cast<int64_t>(p->subs) <= kOrdered;
+  p->join_rows = tiles <= 256 ? 4 : kRowTile;
   p->waves = waves_in(p->c.d, bytes_of, !p->cut && tiles < 256);
   p->resident = 256 * std::max(1, 4 * waves_of(p->c.d, bytes_of, groups) / p->waves);
   p->least = 8 * p->waves;                           // (two steps a wave)
-  // up to p->resident tiles are cut into that many pieces at most, more into half as many more than they are
-  int64_t pieces = std::max<int64_t>(p->resident, tiles + p->resident / 2);
-  pieces = !p->cut ? tiles : std::min(pieces, tiles * (6 * most_steps / p->least + 1));
-  if (pieces > max_groups(64 * kWaves) || tiles > max_groups(kJoinThreads)) return false;
-  p->groups = static_cast<uint32_t>(pieces);
-  const size_t slots = p->cut ? static_cast<size_t>(pieces) * p->tile_rows : 0;
-  *bytes = slots * (p->c.d + 2) * sizeof(float) + (p->cut ? static_cast<size_t>(tiles) * 16 : 0) + 16;
+  p->most_units = static_cast<int>(steps) * (2 + groups);
+  // few tiles are cut into p->resident pieces at most, others into as many more than they are
+  auto pieces_of = [&](int64_t n) { return std::min(n + p->resident, n * (6 * steps / p->least + 2)); };
+  p->groups = p->cut ? pieces_of(tiles) : tiles;
+  // (of more tiles than are cut, as for the most that are: a workspace serves every smaller batch)
+  if (steps <= 64) return 16;
+  const int64_t n = p->cut ? tiles : std::min<int64_t>(tiles, std::max<int64_t>(511, 4 * steps));
+  return static_cast<size_t>(pieces_of(n)) * p->tile_rows * (p->c.d + 2) * sizeof(float) + static_cast<size_t>(n) * 16 + 16;
+}
+
+bool plan_tree(TreeParams* p, size_t* bytes) {
+  p->by_group = Divider(static_cast<uint32_t>(p->group));
+  const int64_t rows = static_cast<int64_t>(p->max_q) * p->group;
+  auto steps_of = [](int64_t span) { return std::max<int64_t>(1, (span + kUnit - 1) / kUnit); };
+  const int64_t all_steps = steps_of(p->max_kv);
+  int64_t steps = all_steps;
+  if (p->window) steps = steps_of(std::min<int64_t>(p->max_kv, static_cast<int64_t>(p->window) + p->max_q + kUnit));
+  // units are counted in 32 bits
+  if (static_cast<int64_t>(p->B) * ((rows + kRowTile - 1) / kRowTile) * p->c.heads * 8 * all_steps > 0x50000000) return false;
+  // Rows share a walk over the tokens where there is work for every compute unit; where there is not, tiles of
+  // fewer rows end sooner.
+  const int most = most_groups(p->c.d, p->dtype == CTS_F32);
+  int groups = 0;
+  *bytes = 0;
+  for (int g = 1; g <= most && (g == 1 || rows > g / 2 * kRowTile); g *= 2) {
+    *bytes = std::max(*bytes, plan_groups(p, g, all_steps));         // (whichever is taken, with any window)
+    const int64_t tiles = static_cast<int64_t>(p->B) * p->subs * p->c.heads;
+    if (tiles + p->resident > max_groups(64 * kWaves) || tiles > max_groups(kJoinThreads)) return false;
+    if (!groups && (tiles * steps <= kLittleWork || rows <= p->tile_rows || 2 * g > most)) groups = g;
+  }
+  plan_groups(p, groups, steps);
   return true;
 }
 

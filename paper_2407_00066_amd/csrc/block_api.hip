@@ -295,6 +295,18 @@ size_t cts_kv_tree_attention_workspace_size(const cts_attn_problem* p, const cts
   return plan(p, c, &a, &bytes) == CTS_OK ? bytes : 0;
 }
 
+int cts_kv_tree_attention_plan(const cts_attn_problem* p, const cts_kv_cache* c, int32_t* how) {
+  cts::TreeParams a{};
+  size_t bytes = 0;
+  const int e = plan(p, c, &a, &bytes);
+  if (e != CTS_OK) return e;
+  if (!how) return CTS_ERR_INVALID_ARG;
+  how[0] = a.tile_rows;
+  how[1] = a.cut ? 2 : a.ordered ? 1 : 0;
+  how[2] = a.waves;
+  return CTS_OK;
+}
+
 int cts_kv_tree_attention(const cts_attn_problem* p, const cts_kv_cache* c, const void* q, int64_t ldq,
                           const int32_t* block_table, const int32_t* kv_len, const int32_t* q_start, const uint32_t* mask,
                           int64_t mask_words, const int32_t* positions, void* out, int64_t ldo, void* workspace,

@@ -91,11 +91,11 @@ struct TreeParams : AttnParams {
   const int32_t* positions;                     // of the rows, with a window
   int tile_rows;
   Divider by_group;
-  // whether tiles are cut along their tokens; workgroups; how many run at a time; units of work of a
-  // piece at least; waves of a workgroup
-  bool cut;
-  uint32_t groups;
-  int resident, least, waves;
+  // whether tiles are cut along their tokens; if not, whether those with most work go first; workgroups; how many run
+  // at a time; units of work of a piece at least, of a tile at most; waves of a workgroup; rows of a workgroup that joins
+  bool cut, ordered;
+  int64_t groups;
+  int resident, least, most_units, waves, join_rows;
 };
 bool plan_tree(TreeParams* p, size_t* bytes);
 void place_tree(TreeParams* p, void* workspace);
