@@ -6,7 +6,9 @@
 // quantised.  Bound by memory like those two; a key is read once from memory
 // instead of twice, and its turned row is not written.  Workgroups take keys, values or queries.
 // A thread has 8 elements of a key: the 8 that they are turned with are another thread's, and
-// read again from the nearest cache instead of exchanged, so that any rot will do.
+// read again from the nearest cache instead of exchanged, so that any rot will do.  8191 tokens of 32 + 8 heads of
+// 128 in bf16: 34.6 us, 5.1 TB/s (rotary and write in turn 38.9); 33 tokens: 4.9 us (7.6), the chain
+// position, angles, key.
 #include "kvblock.h"
 #include "rows.h"
 
@@ -15,29 +17,23 @@ namespace {
 
 struct Append {
   KvCache c;
-  Work work;
+  Work work;                                     // of the values
   RotaryParams r;                                // [0] the queries, [1] the keys (out may be null)
+  Divider per_token;                             // threads of a token's keys
   const void* v; int64_t ldv;
   const int64_t* slots;
-  uint32_t kv_groups;                            // workgroups of keys and values, in turn; then come those of queries
-  int q_threads;
+  uint32_t key_groups, value_groups;             // workgroups of keys and of values; then come those of queries
+  int key_threads, query_threads;
 };
 
-// f[8], eighth e of a key of token t, turned; at: the key's row.
-template <typename T> __device__ __forceinline__ void turn8(const RotaryParams& p, int64_t t, int e, const T* at, float* f) {
-  const int half = p.rot / 2, first = 8 * e;
-  if (first >= p.rot) return;
-  float c[8], s[8];
-  if (p.interleaved) {
-    angles<4>(p, t, first / 2, c, s);
+// f[8], eighth e of a key, turned; g: the eighth that it is turned with (halves).
+template <int N> __device__ __forceinline__ void turn8(const RotaryParams& p, int e, const float* c, const float* s,
+                                                       float* f, const float* g) {
+  if constexpr (N == 4) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) turn(f[2 * j], f[2 * j + 1], c[j], s[j]);
   } else {
-    const bool low = first < half;
-    const int j0 = low ? first : first - half;
-    float g[8];
-    load8(at + (low ? first + half : j0), g);
-    angles<8>(p, t, j0, c, s);
+    const bool low = 8 * e < p.rot / 2;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       float lo = low ? f[j] : g[j], hi = low ? g[j] : f[j];
@@ -58,73 +54,94 @@ __device__ __forceinline__ void round8(bf16_t*, float* f) {
   }
 }
 
-template <typename T, int HEADS, bool NT>
-__global__ __launch_bounds__(kThreads) void kv_append_kernel(Append p) {
-  if (blockIdx.x >= p.kv_groups) {
-    const int i = static_cast<int>(blockIdx.x - p.kv_groups) * kThreads + threadIdx.x;
-    if (i < p.q_threads) turn_heads<T, HEADS, NT>(p.r, 0, i);
-    return;
+// Thread i of the keys: eighth e of HEADS heads of a token, which share its angles.  A head's threads are
+// neighbours in one wave, whose loads are all done before it stores: turned keys may be written over the keys.
+template <typename T, int HEADS, bool NT> __device__ __forceinline__ void append_keys(const Append& p, int i) {
+  const int per = p.c.d >> 3, shift = 31 - __builtin_clz(per), groups = (p.c.heads + HEADS - 1) / HEADS;
+  const int64_t t = p.per_token(i);
+  const int in_token = i - static_cast<int>(t) * p.per_token.d, group = in_token >> shift, e = in_token & (per - 1);
+  const int64_t slot = p.slots[t];
+  const T* const row = static_cast<const T*>(p.r.in[1]) + t * p.r.ldi[1];
+  const int half = p.r.rot / 2, first = 8 * e;
+  const bool turns = first < p.r.rot, pairs = turns && !p.r.interleaved;
+  float f[HEADS][8], g[HEADS][8];
+#pragma unroll
+  for (int k = 0; k < HEADS; ++k) {
+    const int head = min(group + k * groups, p.c.heads - 1);
+    load8(row + head * p.c.d + first, f[k]);
+    if (pairs) load8(row + head * p.c.d + (first < half ? first + half : first - half), g[k]);
   }
-  const int64_t t0 = static_cast<int64_t>(blockIdx.x >> 1) * p.work.tokens;
-  const int ne = p.work.ne.d, per = p.c.d >> 3, shift = 31 - __builtin_clz(per);
-  const int n = static_cast<int>(min(static_cast<int64_t>(p.work.tokens), p.r.T - t0)) * ne;
-  const bool value = blockIdx.x & 1;
-  const T* const src = static_cast<const T*>(value ? p.v : p.r.in[1]);
-  const int64_t ld = value ? p.ldv : p.r.ldi[1];
-  // A head's threads are neighbours in one wave, whose loads are all done before it stores:
-  // turned keys may be written over the keys themselves.
-  for (int i0 = threadIdx.x; i0 < n; i0 += kThreads * kPieces) {
-    float f[kPieces][8];
-    int64_t slot[kPieces];
-    int piece[kPieces];
+  if (turns) {
+    float c[8] = {}, s[8] = {};
+    if (p.r.interleaved) {
+      angles<4>(p.r, t, first / 2, c, s);
 #pragma unroll
-    for (int j = 0; j < kPieces; ++j) {
-      const int i = i0 + j * kThreads;           // four threads of a block of 32 go together: 4 | ne and 4 | n
-      slot[j] = -1;
-      if (i >= n) continue;
-      const int64_t t = t0 + p.work.ne(i);
-      piece[j] = i - static_cast<int>(p.work.ne(i)) * ne;
-      slot[j] = p.slots[t];
-      const T* const row = src + t * ld;
-      load8(row + piece[j] * 8, f[j]);
-      if (!value) {
-        const int e = piece[j] & (per - 1);
-        turn8(p.r, t, e, row + (piece[j] - e) * 8, f[j]);
-        round8(static_cast<T*>(nullptr), f[j]);
-      }
+      for (int k = 0; k < HEADS; ++k) turn8<4>(p.r, e, c, s, f[k], g[k]);
+    } else {
+      angles<8>(p.r, t, first < half ? first : first - half, c, s);
+#pragma unroll
+      for (int k = 0; k < HEADS; ++k) turn8<8>(p.r, e, c, s, f[k], g[k]);
     }
+  }
 #pragma unroll
-    for (int j = 0; j < kPieces; ++j) {
-      const int i = i0 + j * kThreads;
-      if (i >= n) continue;
-      if (!value && p.r.out[1]) {
-        T* const o = static_cast<T*>(p.r.out[1]) + (t0 + p.work.ne(i)) * p.r.ldo[1] + piece[j] * 8;
+  for (int k = 0; k < HEADS; ++k) {
+    const int head = group + k * groups;
+    if (head >= p.c.heads) continue;
+    round8(static_cast<T*>(nullptr), f[k]);
+    if (p.r.out[1]) {
+      T* const o = static_cast<T*>(p.r.out[1]) + t * p.r.ldo[1] + head * p.c.d + first;
 #pragma unroll
-        for (int x = 0; x < 8; x += Elem<T>::N) put<T, Elem<T>::N, NT>(o + x, f[j] + x);
-      }
-      if (slot[j] < 0 || slot[j] >= p.c.slots()) continue;
-      store8(p.c, slot[j], piece[j] >> shift, piece[j] & (per - 1), value, f[j]);
+      for (int x = 0; x < 8; x += Elem<T>::N) put<T, Elem<T>::N, NT>(o + x, f[k] + x);
     }
+    if (slot >= 0 && slot < p.c.slots()) store8(p.c, slot, head, e, false, f[k]);
   }
 }
 
-// Workgroups of a call's queries; more than this many threads are not counted in 31 bits.
-constexpr int64_t kMostQuery = 0x7fffff00;
+template <typename T, int HEADS, bool NT>
+__global__ __launch_bounds__(kThreads) void kv_append_kernel(Append p) {
+  uint32_t w = blockIdx.x;
+  if (w < p.key_groups) {
+    const int i = static_cast<int>(w) * kThreads + threadIdx.x;
+    if (i < p.key_threads) append_keys<T, HEADS, NT>(p, i);
+    return;
+  }
+  w -= p.key_groups;
+  if (w < p.value_groups) {
+    write_rows<T>(p.c, p.work, p.r.T, w, static_cast<const T*>(p.v), p.ldv, p.slots, true);
+    return;
+  }
+  const int i = static_cast<int>(w - p.value_groups) * kThreads + threadIdx.x;
+  if (i < p.query_threads) turn_heads<T, HEADS, NT>(p.r, 0, i);
+}
+
+// Threads are counted in 31 bits.
+constexpr int64_t kMostThreads = 0x7fffff00;
+int64_t key_threads(const KvCache& c, int T, int heads) { return static_cast<int64_t>(T) * ((c.heads + heads - 1) / heads) * (c.d >> 3); }
 int64_t query_threads(const RotaryParams& r) { return static_cast<int64_t>(r.T) * (r.heads[0] ? r.per_token.d : 0); }
+int64_t groups_for(int64_t threads) { return (threads + kThreads - 1) / kThreads; }
 
 template <typename T, int HEADS, bool NT> hipError_t append_launch(Append p, hipStream_t s) {
   if (p.r.heads[0]) set_threads<HEADS>(&p.r);
-  p.q_threads = static_cast<int>(query_threads(p.r));
-  const uint32_t q_groups = static_cast<uint32_t>((static_cast<int64_t>(p.q_threads) + kThreads - 1) / kThreads);
-  kv_append_kernel<T, HEADS, NT><<<p.kv_groups + q_groups, kThreads, 0, s>>>(p);
+  p.query_threads = static_cast<int>(query_threads(p.r));
+  p.key_threads = static_cast<int>(key_threads(p.c, p.r.T, HEADS));
+  p.per_token = Divider(static_cast<uint32_t>(p.key_threads / p.r.T));
+  p.key_groups = static_cast<uint32_t>(groups_for(p.key_threads));
+  p.value_groups = static_cast<uint32_t>(groups_of(p.work, p.r.T));
+  const uint32_t all = p.key_groups + p.value_groups + static_cast<uint32_t>(groups_for(p.query_threads));
+  kv_append_kernel<T, HEADS, NT><<<all, kThreads, 0, s>>>(p);
   return hipGetLastError();
 }
 
 template <typename T> hipError_t append_typed(const Append& p, hipStream_t s) {
-  // (the rule of rotary)
-  constexpr int64_t kShared = kThreads * 4 * 1024;
-  if (static_cast<int64_t>(p.r.T) * p.r.heads[0] * (p.r.d / 16) < kShared) return append_launch<T, 1, false>(p, s);
-  return append_launch<T, 4, true>(p, s);
+  // Heads share their angles where that leaves workgroups enough: 8191 tokens of 32 + 8 heads of 128 in bf16, the
+  // keys' threads with one head each and with four, 36.1 / 34.6 us; 2003 of 20 + 4 in fp32, one head and
+  // ordinary stores, two and stores past the caches, 17.3 / 13.2.
+  const int64_t n = static_cast<int64_t>(p.r.T) * (p.r.heads[0] * (p.r.d / 16) + p.c.heads * (p.r.d / 8));
+  constexpr int64_t kShared = kThreads * 1024;
+  const bool nt = sizeof(T) * p.r.T * p.r.heads[0] * p.r.d >= kStreamBytes;
+  if (n >= 4 * kShared) return nt ? append_launch<T, 4, true>(p, s) : append_launch<T, 4, false>(p, s);
+  if (n >= kShared) return nt ? append_launch<T, 2, true>(p, s) : append_launch<T, 2, false>(p, s);
+  return append_launch<T, 1, false>(p, s);
 }
 
 // ------------------------------------------------------------------- keep
@@ -185,15 +202,16 @@ __global__ __launch_bounds__(kKeepThreads) void kv_keep_kernel(KvCache c, int ma
 bool append_fits(const KvCache& c, const RotaryParams& r) {
   RotaryParams one = r;
   if (r.heads[0]) set_threads<1>(&one);
-  const int64_t q = query_threads(one);
-  return q <= kMostQuery && 2 * groups_of(work_of(c, r.T), r.T) + (q + kThreads - 1) / kThreads <= max_groups(kThreads);
+  const int64_t q = query_threads(one), k = key_threads(c, r.T, 1);
+  return q <= kMostThreads && k <= kMostThreads &&
+         groups_for(q) + groups_for(k) + groups_of(work_of(c, r.T), r.T) <= max_groups(kThreads);
 }
 
 hipError_t launch_kv_append(const KvCache& c, const RotaryParams& r, const void* v, int64_t ldv, const int64_t* slots,
                             int dtype, hipStream_t s) {
-  Append p{c, work_of(c, r.T), r, v, ldv, slots, 0, 0};
-  p.kv_groups = static_cast<uint32_t>(2 * groups_of(p.work, r.T));
-  p.r.heads[1] = 0;                              // (the keys' workgroups take them)
+  Append p{};
+  p.c = c; p.work = work_of(c, r.T); p.r = r; p.v = v; p.ldv = ldv; p.slots = slots;
+  p.r.heads[1] = 0;                              // (their workgroups take them)
   return dtype == CTS_F32 ? append_typed<float>(p, s) : append_typed<bf16_t>(p, s);
 }
 

@@ -75,6 +75,36 @@ __device__ __forceinline__ void store8(const KvCache& c, int64_t slot, int head,
   if ((e & 3) == 0) (value ? c.vs : c.ks)[at.scale] = static_cast<uint8_t>(s);
 }
 
+// Workgroup w's keys or values of the rows from `rows` on, `ld` apart, into their slots.
+template <typename TI>
+__device__ __forceinline__ void write_rows(const KvCache& c, const Work& work, int T, uint32_t w, const TI* __restrict__ rows,
+                                           int64_t ld, const int64_t* __restrict__ slots, bool value) {
+  const int64_t t0 = static_cast<int64_t>(w) * work.tokens;
+  const int ne = work.ne.d, per = c.d >> 3, shift = 31 - __builtin_clz(per);
+  const int n = static_cast<int>(min(static_cast<int64_t>(work.tokens), T - t0)) * ne;
+  const TI* const src = rows + t0 * ld;
+  for (int i0 = threadIdx.x; i0 < n; i0 += kThreads * kPieces) {
+    float f[kPieces][8];
+    int64_t slot[kPieces];
+    int piece[kPieces];
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) {
+      const int i = i0 + j * kThreads;           // four threads of a block of 32 go together: 4 | ne and 4 | n
+      slot[j] = -1;
+      if (i >= n) continue;
+      const int t = work.ne(i);
+      piece[j] = i - t * ne;
+      slot[j] = slots[t0 + t];
+      load8(src + static_cast<uint64_t>(static_cast<uint32_t>(t)) * static_cast<uint32_t>(ld) + piece[j] * 8, f[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) {
+      if (slot[j] < 0 || slot[j] >= c.slots()) continue;
+      store8(c, slot[j], piece[j] >> shift, piece[j] & (per - 1), value, f[j]);
+    }
+  }
+}
+
 // Enough workgroups for every compute unit first, then kPieces pieces a thread.
 Work work_of(const KvCache& c, int T, int elements = 8) {
   const int64_t ne = static_cast<int64_t>(c.heads) * c.d / elements;

@@ -17,32 +17,8 @@ template <typename TI>
 __global__ __launch_bounds__(kThreads) void kv_write_kernel(KvCache c, Work work, int T, const TI* __restrict__ k,
                                                             int64_t ldk, const TI* __restrict__ v, int64_t ldv,
                                                             const int64_t* __restrict__ slots) {
-  const int64_t t0 = static_cast<int64_t>(blockIdx.x) * work.tokens;
-  const int ne = work.ne.d, per = c.d >> 3, shift = 31 - __builtin_clz(per);
-  const int n = static_cast<int>(min(static_cast<int64_t>(work.tokens), T - t0)) * ne;
   const bool value = blockIdx.y;
-  const TI* const src = value ? v + t0 * ldv : k + t0 * ldk;
-  const int64_t ld = value ? ldv : ldk;
-  for (int i0 = threadIdx.x; i0 < n; i0 += kThreads * kPieces) {
-    float f[kPieces][8];
-    int64_t slot[kPieces];
-    int piece[kPieces];
-#pragma unroll
-    for (int j = 0; j < kPieces; ++j) {
-      const int i = i0 + j * kThreads;           // four threads of a block of 32 go together: 4 | ne and 4 | n
-      slot[j] = -1;
-      if (i >= n) continue;
-      const int t = work.ne(i);
-      piece[j] = i - t * ne;
-      slot[j] = slots[t0 + t];
-      load8(src + static_cast<uint64_t>(static_cast<uint32_t>(t)) * static_cast<uint32_t>(ld) + piece[j] * 8, f[j]);
-    }
-#pragma unroll
-    for (int j = 0; j < kPieces; ++j) {
-      if (slot[j] < 0 || slot[j] >= c.slots()) continue;
-      store8(c, slot[j], piece[j] >> shift, piece[j] & (per - 1), value, f[j]);
-    }
-  }
+  write_rows<TI>(c, work, T, blockIdx.x, value ? v : k, value ? ldv : ldk, slots, value);
 }
 
 // Read back: a thread writes 16 bytes, so that a wave's stores are whole lines: 8 elements
