@@ -7,8 +7,8 @@
 // instead of twice, and its turned row is not written.  Workgroups take keys, values or queries.
 // A thread has 8 elements of a key: the 8 that they are turned with are another thread's, and
 // read again from the nearest cache instead of exchanged, so that any rot will do.  8191 tokens of 32 + 8 heads of
-// 128 in bf16: 34.6 us, 5.1 TB/s (rotary and write in turn 38.9); 33 tokens: 4.9 us (7.6), the chain
-// position, angles, key.
+// 128 in bf16: 33.3 us, 5.3 TB/s (rotary and write 29.5 + 9.4); 33 tokens: 4.9 us on the GPU
+// (5.1 + 2.5), the chain of position, angles and rows.
 #include "kvblock.h"
 #include "rows.h"
 
@@ -133,15 +133,13 @@ template <typename T, int HEADS, bool NT> hipError_t append_launch(Append p, hip
 }
 
 template <typename T> hipError_t append_typed(const Append& p, hipStream_t s) {
-  // Heads share their angles where that leaves workgroups enough: 8191 tokens of 32 + 8 heads of 128 in bf16, the
-  // keys' threads with one head each and with four, 36.1 / 34.6 us; 2003 of 20 + 4 in fp32, one head and
-  // ordinary stores, two and stores past the caches, 17.3 / 13.2.
+  // Two heads share their angles where that leaves workgroups enough, and large outputs are stored past the caches.
+  // 32 + 8 heads of 128 in bf16, 1, 2 and 4 heads a thread: 200 tokens 5.0 / 5.7 / 5.9 us, 600 8.1 / 5.4 / 6.1, 2000 16.9
+  // / 8.9 / 9.1, 8191 55.9 / 33.3 / 34.0 (with ordinary stores 58.7 / 33.7 / 35.2).
   const int64_t n = static_cast<int64_t>(p.r.T) * (p.r.heads[0] * (p.r.d / 16) + p.c.heads * (p.r.d / 8));
-  constexpr int64_t kShared = kThreads * 1024;
-  const bool nt = sizeof(T) * p.r.T * p.r.heads[0] * p.r.d >= kStreamBytes;
-  if (n >= 4 * kShared) return nt ? append_launch<T, 4, true>(p, s) : append_launch<T, 4, false>(p, s);
-  if (n >= kShared) return nt ? append_launch<T, 2, true>(p, s) : append_launch<T, 2, false>(p, s);
-  return append_launch<T, 1, false>(p, s);
+  if (n < 512 * kThreads) return append_launch<T, 1, false>(p, s);
+  if (sizeof(T) * p.r.T * p.r.heads[0] * p.r.d < kStreamBytes) return append_launch<T, 2, false>(p, s);
+  return append_launch<T, 2, true>(p, s);
 }
 
 // ------------------------------------------------------------------- keep
