@@ -51,6 +51,14 @@ __device__ __forceinline__ TreeTile uniform(TreeTile t) {
           __builtin_amdgcn_readfirstlane(t.steps)};
 }
 
+__device__ __forceinline__ TreeTile of_lane(const TreeTile& t, int lane) {
+  return {__builtin_amdgcn_readlane(t.b, lane),      __builtin_amdgcn_readlane(t.q0, lane),
+          __builtin_amdgcn_readlane(t.drafts, lane), __builtin_amdgcn_readlane(t.rows, lane),
+          __builtin_amdgcn_readlane(t.row0, lane),   __builtin_amdgcn_readlane(t.past, lane),
+          __builtin_amdgcn_readlane(t.lo, lane),     __builtin_amdgcn_readlane(t.hi, lane),
+          __builtin_amdgcn_readlane(t.steps, lane)};
+}
+
 // Kinds of instructions to the scheduler.
 constexpr int kValu = 0x2, kMatrix = 0x8, kLdsRead = 0x100;
 
@@ -191,13 +199,14 @@ __device__ __forceinline__ int look_up(const TreeParams& p, int b, int lo, int s
   return p.table[static_cast<int64_t>(b) * p.max_pages + min(tok >> p.c.page_shift, static_cast<int64_t>(p.max_pages - 1))];
 }
 
-// Word w of the tile's query q as it stands in shared memory: drafts that do not count are 0.
-__device__ __forceinline__ uint32_t mask_word(const TreeParams& p, const TreeTile& t, int first, int q, int w) {
-  if (w < 0) return ~0u;
+// Word w of the mask of the tile's query q as it is loaded (from the last draft's words on: the last one that counts),
+// and as it stands in shared memory: drafts that do not count are 0.
+__device__ __forceinline__ uint32_t load_mask(const TreeParams& p, const TreeTile& t, int first, int q, int w) {
+  return p.mask[static_cast<int64_t>(t.q0 + first + q) * p.mask_words + min(max(w, 0), (t.drafts - 1) >> 5)];
+}
+__device__ __forceinline__ uint32_t mask_word(const TreeTile& t, int w, uint32_t bits) {
   const int left = t.drafts - 32 * w;
-  if (left <= 0) return 0;
-  const uint32_t bits = p.mask[static_cast<int64_t>(t.q0 + first + q) * p.mask_words + w];
-  return left < 32 ? bits & ((1u << left) - 1) : bits;
+  return w < 0 ? ~0u : left <= 0 ? 0u : left < 32 ? bits & ((1u << left) - 1) : bits;
 }
 
 // 32 bytes from `at` and from 1, 2 and 3 times STRIDE further on, added element by element to f (in one piece with
@@ -304,24 +313,19 @@ __device__ __forceinline__ void attend(const TreeParams& p, const TreeTile& t, i
   const int q_first = p.by_group(t.row0), q_last = p.by_group(min(t.rows, t.row0 + RG * kRowTile) - 1);
   const int words = (q_last - q_first + 1) * kMaskWords;
   uint32_t word = 0;
-  if (static_cast<int>(threadIdx.x) < words) word = mask_word(p, t, q_first, threadIdx.x / kMaskWords, static_cast<int>(threadIdx.x % kMaskWords) - 1);
+  if (static_cast<int>(threadIdx.x) < words) word = load_mask(p, t, q_first, threadIdx.x / kMaskWords, static_cast<int>(threadIdx.x % kMaskWords) - 1);
   bf16x8 qf[Q::kShared ? 1 : RG][KS][NS];
-  auto query_at = [&](int r, bool* live) -> const TQ* {
-    const int row = t.row0 + kRowTile * r + n, query = p.by_group(row);
-    *live = row < t.rows;
-    return static_cast<const TQ*>(p.q) + (*live ? (t.q0 + query) * p.ldq +
-                                          static_cast<int64_t>(h * p.group + row - query * p.group) * D : 0) + (D / 4) * g;
-  };
   constexpr int kMine = Q::kShared ? (RG * KS + stride - 1) / stride : RG * KS;      // the waves share out what they share
-  float f[kMine][8];
+  uint4 raw[kMine][sizeof(TQ) / 2];
+  auto row_of = [&](int k) { return t.row0 + kRowTile * min((Q::kShared ? wave + k * stride : k) / KS, RG - 1) + n; };
 #pragma unroll
   for (int k = 0; k < kMine; ++k) {
-    const int i = Q::kShared ? wave + k * stride : k, r = i / KS, s = i - r * KS;
-    bool live;
-    const TQ* const q = query_at(min(r, RG - 1), &live);
+    const int s = (Q::kShared ? wave + k * stride : k) % KS;
+    const int row = min(row_of(k), t.rows - 1), query = p.by_group(row);               // (rows that are not there: 0 later)
+    const TQ* const q = static_cast<const TQ*>(p.q) + (t.q0 + query) * p.ldq +
+                        static_cast<int64_t>(h * p.group + row - query * p.group) * D + (D / 4) * g + 8 * s;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[k][e] = 0.0f;
-    if (live) load_q(q + 8 * s, f[k]);
+    for (int e = 0; e < static_cast<int>(sizeof(TQ) / 2); ++e) raw[k][e] = reinterpret_cast<const uint4*>(q)[e];
   }
   // of row `lane`: its query's place among the tile's, and the first token before the drafts that it sees
   int2 seer = make_int2(0, 0);
@@ -334,21 +338,25 @@ __device__ __forceinline__ void attend(const TreeParams& p, const TreeTile& t, i
 #pragma unroll
     for (int i = 0; i < S::kSlots - 1; ++i) ask(min(i, count - 1));
   for (int k = threadIdx.x; k < words; k += 64 * stride) {
-    if (k >= 64 * stride) word = mask_word(p, t, q_first, k / kMaskWords, k % kMaskWords - 1);
-    masks[k / kMaskWords][k % kMaskWords] = word;
+    if (k >= 64 * stride) word = load_mask(p, t, q_first, k / kMaskWords, k % kMaskWords - 1);
+    masks[k / kMaskWords][k % kMaskWords] = mask_word(t, k % kMaskWords - 1, word);
   }
   if (threadIdx.x < RG * kRowTile) seers[threadIdx.x] = seer;           // (the first wave's)
 #pragma unroll
   for (int k = 0; k < kMine; ++k) {
-    if constexpr (Q::kShared) {
-      const int i = wave + k * stride;
-      bf16x8 part[NS];
-      split<NS>(f[k], part);
-      if (i < RG * KS)
+    if (row_of(k) >= t.rows)
 #pragma unroll
-        for (int z = 0; z < NS; ++z) queries[i * NS + z][lane] = part[z];
-    } else {
-      split<NS>(f[k], qf[k / KS][k % KS]);
+      for (int e = 0; e < static_cast<int>(sizeof(TQ) / 2); ++e) raw[k][e] = make_uint4(0, 0, 0, 0);
+    bf16x8 part[NS];
+    if constexpr (NS == 1) part[0] = __builtin_bit_cast(bf16x8, raw[k][0]);
+    else split<NS>(reinterpret_cast<const float*>(&raw[k][0]), part);
+#pragma unroll
+    for (int z = 0; z < NS; ++z) {
+      if constexpr (Q::kShared) {
+        if (wave + k * stride < RG * KS) queries[(wave + k * stride) * NS + z][lane] = part[z];
+      } else {
+        qf[k / KS][k % KS][z] = part[z];
+      }
     }
   }
 #pragma unroll
@@ -676,11 +684,7 @@ __device__ __forceinline__ bool find_piece(const TreeParams& p, int w, Piece* ou
     if (!here) return false;
     out->slot = w;
   }
-  out->t = {__builtin_amdgcn_readlane(t.b, at),      __builtin_amdgcn_readlane(t.q0, at),
-            __builtin_amdgcn_readlane(t.drafts, at), __builtin_amdgcn_readlane(t.rows, at),
-            __builtin_amdgcn_readlane(t.row0, at),   __builtin_amdgcn_readlane(t.past, at),
-            __builtin_amdgcn_readlane(t.lo, at),     __builtin_amdgcn_readlane(t.hi, at),
-            __builtin_amdgcn_readlane(t.steps, at)};
+  out->t = of_lane(t, at);
   mine = __builtin_amdgcn_readlane(mine, at);
   out->h = mine == 1 ? of : of / mine;
   // (a multiple of its waves' number: they end together)
@@ -698,20 +702,18 @@ __device__ __forceinline__ bool find_piece(const TreeParams& p, int w, Piece* ou
 // The tile (of a head) whose work is the rank-th most, to an eighth of the most there can be; of up to kOrdered tiles.
 // With more workgroups than compute units the longest go first: they would end last.
 constexpr int kOrdered = 256;
-__device__ __forceinline__ int tile_of_rank(const TreeParams& p, int rank) {
+__device__ __forceinline__ TreeTile tile_of_rank(const TreeParams& p, int rank) {
   constexpr int kEach = kOrdered / 64;
   const int lane = threadIdx.x & 63, tiles = p.B * p.subs;
   const float scale = 8.0f / static_cast<float>(p.most_units);
+  TreeTile t[kEach]{};
   int bucket[kEach];
 #pragma unroll
-  for (int c = 0; c < kEach; ++c) {
-    const int i = 64 * c + lane;
-    bucket[c] = -1;
-    if (i < tiles) {
-      const TreeTile t = tile_at(p, i);
-      bucket[c] = min(7, static_cast<int>(static_cast<float>(t.steps * unit_of(t, p.tile_rows)) * scale));
-    }
-  }
+  for (int c = 0; c < kEach; ++c)
+    if (64 * c + lane < tiles) t[c] = tile_at(p, 64 * c + lane);
+#pragma unroll
+  for (int c = 0; c < kEach; ++c)
+    bucket[c] = 64 * c + lane < tiles ? min(7, static_cast<int>(static_cast<float>(t[c].steps * unit_of(t[c], p.tile_rows)) * scale)) : -1;
   for (int k = 7; k >= 0; --k)
 #pragma unroll
     for (int c = 0; c < kEach; ++c) {
@@ -719,11 +721,11 @@ __device__ __forceinline__ int tile_of_rank(const TreeParams& p, int rank) {
       const int n = __builtin_popcountll(here);
       if (rank < n) {
         const int below = __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(here >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(here), 0));
-        return 64 * c + __builtin_ctzll(__ballot(bucket[c] == k && below == rank));
+        return of_lane(t[c], __builtin_ctzll(__ballot(bucket[c] == k && below == rank)));
       }
       rank -= n;
     }
-  return 0;                                          // (every tile is in a bucket)
+  return TreeTile{};                                 // (every tile is in a bucket)
 }
 
 template <int D, typename TQ>
@@ -823,15 +825,18 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(D, sizeof(TQ), RG)) void tree_
     if (!find_piece(p, w, &me)) return;
     pages = look_up(p, me.t.b, me.t.lo, me.begin + wave, WAVES);
   } else {
-    int index = w / p.c.heads;
+    const int index = w / p.c.heads;
     me.h = w - index * p.c.heads;
-    // the first pages are on their way while the tile's length is
-    if (p.ordered) index = tile_of_rank(p, index);
-    const int b = p.subs == 1 ? index : index / p.subs;
-    if (!p.window) pages = look_up(p, b, 0, wave, WAVES);
-    me.t = uniform(tree_tile(p, b, index - b * p.subs));
+    if (p.ordered) {
+      me.t = tile_of_rank(p, index);
+    } else {
+      const int b = p.subs == 1 ? index : index / p.subs;
+      // the first pages are on their way while the tile's length is
+      if (!p.window) pages = look_up(p, b, 0, wave, WAVES);
+      me.t = uniform(tree_tile(p, b, index - b * p.subs));
+    }
     if (me.t.steps == 0) return;
-    if (p.window) pages = look_up(p, b, me.t.lo, wave, WAVES);
+    if (p.ordered || p.window) pages = look_up(p, me.t.b, me.t.lo, wave, WAVES);
     me.begin = me.slot = 0;
     me.end = me.t.steps;
   }
