@@ -95,6 +95,7 @@ template <int D> struct Step {
   static constexpr int kScales = D == 256 ? 2 : 1;           // loads of 4 bytes a lane for the scales
   static constexpr int kLoads = 2 * kPieces + kScales;
   static constexpr int kBytes = 2 * kPieces * 1024 + kScales * 256;
+  // (three: 200 small trees 63 -> 72 us, 64 x 8 drafts after 4000 tokens 68 -> 76; four: one workgroup a compute unit, 239 -> 370 over long documents)
   static constexpr int kSlots = 2;
 };
 
@@ -806,6 +807,7 @@ __device__ __forceinline__ void take(const TreeParams& p, const Piece& me, int p
 
 // Waves of a workgroup: eight where there are few, four, of which a compute unit takes more, where there are
 // many; shared memory holds the codes of eight waves of heads of 256, and queries in 32 bits beside those of four.
+// One tree over 709 tokens, eight waves or four: 8.8 / 9.5 us, eight in fp32 13.8 / 16.3; 200 small trees 93 / 63, 64 uneven ones 60 / 57.
 constexpr int waves_in(int d, int bytes, bool few) { return d == 256 ? (bytes == 4 ? 4 : 8) : few ? 8 : 4; }
 // Waves of a SIMD that the registers are for.
 constexpr int waves_of(int d, int bytes, int rg) {
@@ -915,8 +917,10 @@ template <int D, typename TQ, int RG> void launch_tiles(const TreeParams& p, hip
     tree_join_kernel<D, TQ><<<dim3(static_cast<uint32_t>(p.B * p.subs * p.c.heads), p.tile_rows / p.join_rows), kJoinThreads, 0, s>>>(p);
 }
 
-// Steps of all tiles up to which tiles of fewer rows are taken.
-constexpr int64_t kLittleWork = 8192;
+// Steps of all tiles up to which tiles of fewer rows are taken (32 + 8 heads of 128, us with tiles of 64 rows / with this: 16
+// sequences of 16 drafts after 2000 tokens 28.1 / 22.5, 200 drafts after 1500 25.9 / 17.8, 8 x 16 in fp32 28.3 / 23.6; above it rows
+// have to share their steps: 64 x 8 after 900 20.9 / 24.0, 64 uneven trees 57 / 63, wide trees 58 / 75, 131 022 tokens 239 / 427).
+constexpr int64_t kLittleWork = 16384;
 
 template <int D, typename TQ> hipError_t launch(const TreeParams& p, hipStream_t s) {
   constexpr int kMost = most_groups(D, sizeof(TQ) == 4);
@@ -937,8 +941,13 @@ static size_t plan_groups(TreeParams* p, int groups, int64_t steps) {
   p->tile_rows = groups * kRowTile;
   p->subs = static_cast<int>((rows + p->tile_rows - 1) / p->tile_rows);
   const int64_t tiles = static_cast<int64_t>(p->B) * p->subs * p->c.heads;
+  // Cut and whole, us: 12 sequences of up to 6000 tokens for one head of 256 24.6 / 56, 8 wide trees 58 / 93, 64 drafts after 8000 tokens
+  // 29 / 73, long documents 239 / 1013; with 512 tiles of up to 128 steps finding the pieces and joining them
+  // costs more than uneven ends: 51.6 / 45.
   p->cut = steps > 64 && (tiles < 512 || steps > std::min<int64_t>(256, tiles / 4));
+  // (64 trees after 40 to 4000 tokens: 64 us in the batch's order, so 57)
   p->ordered = !p->cut && tiles > 256 && p->B * static_cast<int64_t>(p->subs) <= kOrdered;
+  // (64 drafts after 8000 tokens, four rows of a tile a workgroup or 16: 29.4 / 32.3 us; 12 sequences with a head of 256 24.6 / 28.7)
   p->join_rows = tiles <= 256 ? 4 : kRowTile;
   p->waves = waves_in(p->c.d, bytes_of, !p->cut && tiles < 256);
   p->resident = 256 * std::max(1, 4 * waves_of(p->c.d, bytes_of, groups) / p->waves);
