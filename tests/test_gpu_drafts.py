@@ -156,3 +156,57 @@ def test_command_times_drafts(capsys):
     for bad in ("-1", "513"):
         with pytest.raises(SystemExit):
             decoder.main(["--drafts", bad])
+
+
+def test_a_captured_step():
+    """Stored, attended to and cut back in one graph: replays with other tokens, lengths, masks and paths equal eager
+    calls, with eager work between."""
+    rng = np.random.default_rng(3)
+    page, cols, n, kvh, heads, d = 16, 40, [12, 7, 30], 2, 8, 128
+    T, start = sum(n), i32(np.concatenate(([0], np.cumsum(n))).astype(np.int32))
+    table = np.arange(3 * cols, dtype=np.int32).reshape(3, cols)
+    cos, sin = decoder.rotary_table(700, d)
+    cache, other = (cts.kv_cache(3 * cols, page, kvh, d) for _ in range(2))
+    q, k, v = (torch.zeros(T, h, d, dtype=torch.bfloat16, device="cuda") for h in (heads, kvh, kvh))
+    slots, pos = torch.zeros(T, dtype=torch.int64, device="cuda"), torch.zeros(T, dtype=torch.int32, device="cuda")
+    mask, n_kv = torch.zeros(T, 1, dtype=torch.int32, device="cuda"), i32(np.array(n, np.int32))
+    path, n_path = torch.zeros(3, 5, dtype=torch.int32, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
+    tables, out = i32(table), torch.empty_like(q)
+    ws = torch.empty(cts.kv_tree_attention_workspace_size(q, cache, 3, 30, cols * page), dtype=torch.uint8, device="cuda")
+
+    def step(kv, o):
+        turned = cts.kv_append(kv, q, k, v, slots, cos, sin, pos)
+        cts.kv_tree_attention(turned, kv, tables, n_kv, mask, q_start=start, max_q=30, out=o, workspace=ws)
+        cts.kv_keep(kv, tables, n_kv, start, path, n_path)
+
+    for a in (cache.k_codes, cache.v_codes):
+        a.random_(0, 256)
+    for a in (cache.k_scales, cache.v_scales):
+        a.random_(122, 128)
+    step(cache, out)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step(cache, out)
+    for i in range(3):
+        past = rng.integers(0, 600, 3)
+        at = [[table[b][t // page] * page + t % page for t in range(past[b], past[b] + n[b])] for b in range(3)]
+        slots.copy_(torch.tensor(sum(at, [])))
+        n_kv.copy_(torch.from_numpy((past + n).astype(np.int32)))
+        pos.copy_(torch.from_numpy(np.concatenate([past[b] + np.arange(n[b]) // 2 for b in range(3)]).astype(np.int32)))
+        mask.copy_(torch.from_numpy(rng.integers(0, 2 ** 32, (T, 1), dtype=np.uint32).view(np.int32)))
+        path.copy_(torch.from_numpy(rng.integers(0, 7, (3, 5)).astype(np.int32)))
+        n_path.copy_(torch.from_numpy(rng.integers(0, 6, 3).astype(np.int32)))
+        for t in (q, k, v):
+            t.copy_(torch.randn(t.shape, device="cuda"))
+        for a, b in zip((cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales),
+                        (other.k_codes, other.k_scales, other.v_codes, other.v_scales)):
+            b.copy_(a)
+        say("a captured step, replay %d" % i)
+        g.replay()
+        torch.cuda.synchronize()
+        want = torch.empty_like(q)
+        step(other, want)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+        assert all(np.array_equal(a, b) for a, b in zip(to_host(cache), to_host(other)))

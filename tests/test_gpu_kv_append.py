@@ -148,3 +148,21 @@ def test_refusals():
         with pytest.raises(error):
             cts.kv_append(cache, *args, **kw)
     assert all(np.array_equal(a, b) for a, b in zip(to_host(cache), before))
+
+
+@pytest.mark.parametrize("heads,kvh,dtype", [(7, 3, "bf16"), (0, 5, "bf16"), (9, 1, "f32")])
+def test_odd_heads_of_many_tokens_in_place(heads, kvh, dtype):
+    """Threads that take two heads where one is left over: rows are turned in place, on a stream of their own."""
+    T = 6001
+    rows, slots, pos, sections, cache, (cos, sin) = _inputs(T, heads, kvh, 128, 128, 1, 16, dtype, T + heads)
+    q, k, v = rows[:, :heads] if heads else None, rows[:, heads:heads + kvh], rows[:, heads + kvh:]
+    other, before = _copy(cache), rows.clone()
+    say("kv_append of %d tokens, heads %d and %d" % (T, heads, kvh))
+    want_q, want_k = cts.rotary(q, k, cos, sin, pos, sections=sections)
+    cts.kv_write(other, want_k, v, slots)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        cts.kv_append(cache, q, k, v, slots, cos, sin, pos, sections=sections, q_out=q, k_out=k)
+    torch.cuda.synchronize()
+    assert torch.equal(k, want_k) and torch.equal(v, before[:, heads + kvh:]) and _same(cache, other)
+    assert not heads or torch.equal(q, want_q)

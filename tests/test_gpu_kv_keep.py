@@ -120,3 +120,17 @@ def test_refusals():
         args[i] = bad
         with pytest.raises(error):
             cts.kv_keep(cache, *args)
+
+
+def test_unsorted_counts_and_padded_batches():
+    """Sequences without drafts, with counts that fall, and lengths below their drafts: what is no draft's place stays."""
+    cache = cts.kv_cache(6, 16, 2, 64)
+    for a in (cache.k_codes, cache.v_codes, cache.k_scales, cache.v_scales):
+        a.random_(0, 250)
+    before = [a.copy() for a in to_host(cache)]
+    t = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    say("kv_keep of padded batches")
+    # no drafts; starts that fall back; 3 tokens cached of 5 drafts: draft 4 (token 2) to draft 1's place (before the first token)
+    cts.kv_keep(cache, t([[0, 1], [2, 3], [4, 5]]), t([20, 20, 3]), t([4, 4, 0, 5]), t([[0, 1], [1, 0], [2, 4]]), t([2, 2, 2]))
+    torch.cuda.synchronize()
+    assert all(np.array_equal(a, b) for a, b in zip(to_host(cache), before))
