@@ -11,8 +11,8 @@
 // are one shift wherever the drafts begin.
 //
 // 32 + 8 heads of 128 in bf16: 200 requests of 30 to 2000 tokens with 1 to 6 drafts 59 us, 4.0 TB/s of codes; 64 drafts
-// after 131 022 tokens and two like it 237 us, 829 TFLOP/s, bound by vector instructions beside the matrix
-// instructions: a step of 64 rows is 64 products (1024 cycles) and 267 others (3040 cycles in all with two waves a
+// after 131 022 tokens and two like it 230 us, 853 TFLOP/s, bound by vector instructions beside the matrix
+// instructions: a step of 64 rows is 64 products (1024 cycles) and 267 others (2300 cycles in all with two waves a
 // SIMD).  16 rows a walk, which convert the codes four times as often: 427 us.  One tree of 7
 // over 709 tokens: 8.5 us, the chain of lengths, pages, codes and the waves' join.
 #include <algorithm>
@@ -239,7 +239,8 @@ template <int STRIDE> __device__ __forceinline__ void add_four(uint32_t at, floa
 
 // `count` of the tile's steps from s0, `stride` apart, for key/value head h, by
 // wave `wave`; pages: look_up of the first 32.  The workgroup meets once, for masks and queries.
-template <int D, typename TQ, int RG, int stride>
+// SHARED: tiles may have more than 16 rows.
+template <int D, typename TQ, int RG, int stride, bool SHARED>
 __device__ __forceinline__ void attend(const TreeParams& p, const TreeTile& t, int h, int wave, int s0, int count, int pages,
                                        Codes<D, stride>& codes, bf16x8 (*queries)[64], uint32_t (*masks)[kMaskWords], int2* seers, Sums<D>* st) {
   using Q = Query<D, TQ, RG>;
@@ -388,7 +389,16 @@ __device__ __forceinline__ void attend(const TreeParams& p, const TreeTile& t, i
 
   pages = rare(pages);                             // here: waited for inside the loop, the loads under way would be too
   const uint32_t ring_at = __builtin_amdgcn_readfirstlane(lds_at(ring));
+  // Of two waves of a SIMD the older goes first, and the younger of two equal pieces ended a third later, alone for that
+  // time: it goes first every other step (long documents: ends at 177 and 240 us, so at 221 and 232; always: 242 and 179).
+  // (Not where every tile has 16 rows, for whose short steps it costs more than it gives: 8 x 16 drafts after 2000 tokens 18.7 us,
+  // with it 19.5.)
+  const bool younger = SHARED && p.cut && blockIdx.x >= 256;
   for (int it = 0; it < count; ++it) {
+    if (younger) {
+      if (it & 1) __builtin_amdgcn_s_setprio(1);
+      else __builtin_amdgcn_s_setprio(0);
+    }
     const int at = t.lo + (s0 + it * stride) * kUnit;
     // the next step's codes are asked for (past the end: the last step's again); this one's have to be there
     const int next = min(it + S::kSlots - 1, count - 1);
@@ -742,7 +752,7 @@ __device__ __forceinline__ TQ* out_at(const TreeParams& p, int q0, int h, int ro
 }
 
 // The steps of a piece for RG groups of rows, and what comes of them: results, or a cut tile's sums.
-template <int D, typename TQ, int RG, int WAVES>
+template <int D, typename TQ, int RG, int WAVES, bool SHARED>
 __device__ __forceinline__ void take(const TreeParams& p, const Piece& me, int pages, Codes<D, WAVES>& codes,
                                      bf16x8 (*queries)[64], uint32_t (*masks)[kMaskWords], int2* seers) {
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
@@ -750,7 +760,7 @@ __device__ __forceinline__ void take(const TreeParams& p, const Piece& me, int p
   const TreeTile& t = me.t;
   Sums<D> st[RG];
   const int first = me.begin + wave, count = first < me.end ? (me.end - first + WAVES - 1) / WAVES : 0;
-  attend<D, TQ, RG, WAVES>(p, t, me.h, wave, first, count, pages, codes, queries, masks, seers, st);
+  attend<D, TQ, RG, WAVES, SHARED>(p, t, me.h, wave, first, count, pages, codes, queries, masks, seers, st);
   // Each wave brings its sums to the maximum of all, and to their length where the result is whole; then
   // they only have to be added.
   const bool whole = me.end - me.begin == t.steps;
@@ -851,13 +861,13 @@ __global__ __launch_bounds__(64 * WAVES, waves_of(D, sizeof(TQ), RG)) void tree_
   // (groups of rows that the tile does not have are left out)
   const int rows = me.t.rows - me.t.row0;
   if (RG == 1 || rows <= kRowTile) {
-    take<D, TQ, 1, WAVES>(p, me, pages, codes, queries, masks, seers);
+    take<D, TQ, 1, WAVES, (RG > 1)>(p, me, pages, codes, queries, masks, seers);
   } else if constexpr (RG >= 2) {
     if (RG == 2 || rows <= 2 * kRowTile) {
-      take<D, TQ, 2, WAVES>(p, me, pages, codes, queries, masks, seers);
+      take<D, TQ, 2, WAVES, (RG > 1)>(p, me, pages, codes, queries, masks, seers);
     } else if constexpr (RG == 4) {
-      if (rows <= 3 * kRowTile) take<D, TQ, 3, WAVES>(p, me, pages, codes, queries, masks, seers);
-      else take<D, TQ, 4, WAVES>(p, me, pages, codes, queries, masks, seers);
+      if (rows <= 3 * kRowTile) take<D, TQ, 3, WAVES, (RG > 1)>(p, me, pages, codes, queries, masks, seers);
+      else take<D, TQ, 4, WAVES, (RG > 1)>(p, me, pages, codes, queries, masks, seers);
     }
   }
 }
