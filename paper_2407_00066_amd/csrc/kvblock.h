@@ -100,7 +100,29 @@ __device__ __forceinline__ void write_rows(const KvCache& c, const Work& work, i
 #pragma unroll
     for (int j = 0; j < kPieces; ++j) {
       if (slot[j] < 0 || slot[j] >= c.slots()) continue;
-      store8(c, slot[j], piece[j] >> shift, piece[j] & (per - 1), value, f[j]);
+      // (store8's steps once more: called here, the compiler moves 15 registers more a pass, and 8191 tokens of 8 x 128
+      // written and 8704 read take 18.7 us instead of 17.9)
+      // the largest magnitude as an integer: it orders like the value, NaN above all
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(f[j][i]) & 0x7fffffffu);
+      top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 1)));
+      top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 2)));
+      const bool finite = top < 0x7f800000u;
+      // a mantissa from 1.75 on would round past 6: the next power of two then
+      const int s = finite ? min(252, max(1, static_cast<int>((top + (1u << 21)) >> 23) - 2)) : 255;
+      uint32_t q = 0;
+      if (finite) {
+        const float unit = __uint_as_float(static_cast<uint32_t>(s) << 23);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, f[j][0], f[j][1], unit, 0);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, f[j][2], f[j][3], unit, 1);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, f[j][4], f[j][5], unit, 2);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, f[j][6], f[j][7], unit, 3);
+      }
+      const int head = piece[j] >> shift, e = piece[j] & (per - 1);
+      const At at = place(c, slot[j], head, e, value);
+      *reinterpret_cast<uint32_t*>((value ? c.vc : c.kc) + at.code) = q;
+      if ((e & 3) == 0) (value ? c.vs : c.ks)[at.scale] = static_cast<uint8_t>(s);
     }
   }
 }
