@@ -826,12 +826,12 @@ __device__ __forceinline__ void take(const TreeParams& p, const Piece& me, int p
 // One tree over 709 tokens, eight waves or four: 8.8 / 9.5 us, eight in fp32 13.8 / 16.3; 200 small trees 93 / 63, 64 uneven ones 60 / 57.
 constexpr int waves_in(int d, int bytes, bool few) { return d == 256 ? (bytes == 4 ? 4 : 8) : few ? 8 : 4; }
 // Waves of a SIMD that the registers are for.
-constexpr int waves_of(int d, int bytes, int rg) {
-  return d == 256 ? (bytes == 4 ? 1 : 2) : bytes == 4 ? 2 : rg == 1 ? 4 : rg == 2 ? 3 : 2;
+constexpr int waves_of(int d, int bytes, int rg, int waves) {
+  return d == 256 ? (bytes == 4 ? 1 : 2) : bytes == 4 ? 2 : rg == 1 ? 4 : rg == 2 && waves == 4 ? 3 : 2;
 }
 
 template <int D, typename TQ, int RG, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, waves_of(D, sizeof(TQ), RG)) void tree_kernel(TreeParams p) {
+__global__ __launch_bounds__(64 * WAVES, waves_of(D, sizeof(TQ), RG, WAVES)) void tree_kernel(TreeParams p) {
   __shared__ __attribute__((aligned(16))) Codes<D, WAVES> codes;
   __shared__ __attribute__((aligned(16))) bf16x8 queries[Query<D, TQ, RG>::kShared ? Query<D, TQ, RG>::N : 1][64];
   __shared__ uint32_t masks[RG * kRowTile][kMaskWords];
@@ -966,7 +966,7 @@ static size_t plan_groups(TreeParams* p, int groups, int64_t steps) {
   // (64 drafts after 8000 tokens, four rows of a tile a workgroup or 16: 29.4 / 32.3 us; 12 sequences with a head of 256 24.6 / 28.7)
   p->join_rows = tiles <= 256 ? 4 : kRowTile;
   p->waves = waves_in(p->c.d, bytes_of, !p->cut && tiles < 256);
-  p->resident = 256 * std::max(1, 4 * waves_of(p->c.d, bytes_of, groups) / p->waves);
+  p->resident = 256 * std::max(1, 4 * waves_of(p->c.d, bytes_of, groups, p->waves) / p->waves);
   p->least = 8 * p->waves;                           // (two steps a wave)
   p->most_units = static_cast<int>(steps) * (2 + groups);
   // few tiles are cut into p->resident pieces at most, others into as many more than they are
