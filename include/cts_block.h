@@ -188,7 +188,10 @@ int cts_kv_append(const cts_kv_cache* c, int32_t T, int32_t n_q_heads, int32_t r
  * mask is uint32 [T][mask_words], mask_words >= (max_q + 31) / 32; bits past the
  * sequence's drafts are ignored.  A row that sees nothing gives zeros; what no row
  * of a sequence sees never reaches its results.  max_q is at most 512.  Queries past
- * max_q are left out as rows, and as drafts that others see. */
+ * max_q are left out as rows, and as drafts that others see.  Bounds may be loose, with no
+ * limit on their product: the call's launch has room for 2^23 tiles of rows, sequences x
+ * key/value heads x what max_q x (query heads of a key/value head) makes in tiles of 64 (of 32
+ * in f32 or with heads of 256, of 16 with both); more is CTS_ERR_UNSUPPORTED. */
 size_t cts_kv_tree_attention_workspace_size(const cts_attn_problem* p, const cts_kv_cache* c);
 
 /* How a call with these sizes takes its work, for tests and debugging; plan is a host

@@ -612,7 +612,8 @@ struct Piece {
   int h, begin, end, slot;
 };
 
-// Work is counted in units of about 150 cycles: a step takes 2 and one for every group of rows.
+// Work is counted in units of about 150 cycles: a step takes 2 and one for every group of rows. Where bounds
+// allow more of it than 31 bits count, a tile's units are taken 2^unit_shift at a time, rounded up.
 __device__ __forceinline__ int unit_of(const TreeTile& t, int tile_rows) {
   return 2 + (min(t.rows - t.row0, tile_rows) + kRowTile - 1) / kRowTile;
 }
@@ -633,6 +634,7 @@ constexpr int kAround = 100;
 __device__ __forceinline__ bool find_piece(const TreeParams& p, int w, Piece* out) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tiles = p.B * p.subs;
   int4* const info = reinterpret_cast<int4*>(p.info);
+  auto units_of = [&](const TreeTile& t) { return (t.steps * unit_of(t, p.tile_rows) + (1 << p.unit_shift) - 1) >> p.unit_shift; };
   TreeTile t0{};                                     // the first 64 are kept
   int total = 0, some = 0;                           // units, tiles that have any
   for (int base = 0; base < tiles; base += 64) {
@@ -642,7 +644,7 @@ __device__ __forceinline__ bool find_piece(const TreeParams& p, int w, Piece* ou
     if (i < tiles && t.steps == 0 && i % static_cast<int>(gridDim.x) == w && wave == 0)
       for (int h = 0; h < p.c.heads; ++h) info[static_cast<int64_t>(i) * p.c.heads + h] = make_int4(0, 0, 0, 0);
     if (base == 0) t0 = t;
-    total += __builtin_amdgcn_readlane(wave_scan(t.steps * unit_of(t, p.tile_rows)), 63);
+    total += __builtin_amdgcn_readlane(wave_scan(units_of(t)), 63);
     some += __builtin_popcountll(__ballot(t.steps > 0));
   }
   total *= p.c.heads;
@@ -651,10 +653,10 @@ __device__ __forceinline__ bool find_piece(const TreeParams& p, int w, Piece* ou
   const bool few = some <= (tiles <= 64 ? p.resident : p.resident / 2);
   int len;
   if (few) len = (total - 1) / (p.resident - (tiles <= 64 ? some / 2 : some)) + 1;
-  else len = total / p.resident + total / p.resident / 8 + some * (kAround * 5 / 8) / p.resident;
+  else len = total / p.resident + total / p.resident / 8 + (some * (kAround * 5 / 8) / p.resident >> p.unit_shift);
   len = max(len, p.least);
   auto pieces_of = [&](const TreeTile& t) {
-    const int units = t.steps * unit_of(t, p.tile_rows);
+    const int units = units_of(t);
     return units <= len ? (units > 0 ? 1 : 0) : static_cast<int>(static_cast<float>(units) * __builtin_amdgcn_rcpf(static_cast<float>(len))) + 1;
   };
   int at = 0, base = 0, of = 0, mine = 0;            // the tile, and the piece's number among its heads' pieces
@@ -669,7 +671,7 @@ __device__ __forceinline__ bool find_piece(const TreeParams& p, int w, Piece* ou
     if (w >= n) return false;
     const int beside = p.resident - 256;             // (workgroups that have a place beside another)
     of = w < 256 ? w : w < 256 + beside ? n - 1 - (w - 256) : w - beside;
-    const int bucket = mine ? min(7, static_cast<int>(static_cast<float>(t.steps * unit_of(t, p.tile_rows)) *
+    const int bucket = mine ? min(7, static_cast<int>(static_cast<float>(units_of(t)) *
                                                       __builtin_amdgcn_rcpf(static_cast<float>(mine * len)) * 8.0f)) : -1;
     int before = 0;                                  // pieces that come first
 #pragma unroll
@@ -938,6 +940,13 @@ template <int D, typename TQ, int RG> void launch_tiles(const TreeParams& p, hip
 // have to share their steps: 64 x 8 after 900 20.9 / 24.0, 64 uneven trees 57 / 63, wide trees 58 / 75, 131 022 tokens 239 / 427).
 constexpr int64_t kLittleWork = 16384;
 
+// Tiles (of a head) up to which they are cut: every piece is found by a look at all of them, so that finding them
+// takes the square of their number.  6 drafts each after 500 tokens, after 50 to 4000, and after 500 with one sequence of 16 000, bounds of
+// 16 384, 32 + 8 heads of 128, us cut / whole: 512 sequences 127 / 78, 200 / 158, 135 / 163; 1024 309 / 146, 384 / 251, 305 / 205; 2048
+// 839 / 301, 990 / 490, 848 / 297; 8192 9800 / 1290, 9500 / 1840, 9760 / 1140; 4 + 1 heads, 1024 56 / 25, 76 / 61, 66 / 129; 2048
+// 137 / 42, 169 / 89, 144 / 139; 4096 423 / 76, 440 / 142, 429 / 159.
+constexpr int64_t kCutTiles = 2048;
+
 template <int D, typename TQ> hipError_t launch(const TreeParams& p, hipStream_t s) {
   constexpr int kMost = most_groups(D, sizeof(TQ) == 4);
   switch (p.tile_rows / kRowTile) {
@@ -956,25 +965,33 @@ static size_t plan_groups(TreeParams* p, int groups, int64_t steps) {
   const int64_t rows = static_cast<int64_t>(p->max_q) * p->group;
   p->tile_rows = groups * kRowTile;
   p->subs = static_cast<int>((rows + p->tile_rows - 1) / p->tile_rows);
-  const int64_t tiles = static_cast<int64_t>(p->B) * p->subs * p->c.heads;
+  const int64_t of_head = static_cast<int64_t>(p->B) * p->subs;
+  // (more than a launch takes are refused if these tiles are chosen, and only need a workspace that does not fall)
+  const int64_t tiles = std::min(of_head * p->c.heads, max_groups(64 * kWaves));
   // Cut and whole, us: 12 sequences of up to 6000 tokens for one head of 256 24.6 / 56, 8 wide trees 58 / 93, 64 drafts after 8000 tokens
   // 29 / 73, long documents 239 / 1013; with 512 tiles of up to 128 steps finding the pieces and joining them
   // costs more than uneven ends: 51.6 / 45.
-  p->cut = steps > 64 && (tiles < 512 || steps > std::min<int64_t>(256, tiles / 4));
+  p->cut = steps > 64 && of_head <= kCutTiles && (tiles < 512 || steps > std::min<int64_t>(256, tiles / 4));
   // (64 trees after 40 to 4000 tokens: 64 us in the batch's order, so 57)
-  p->ordered = !p->cut && tiles > 256 && p->B * static_cast<int64_t>(p->subs) <= kOrdered;
+  p->ordered = !p->cut && tiles > 256 && of_head <= kOrdered;
   // (64 drafts after 8000 tokens, four rows of a tile a workgroup or 16: 29.4 / 32.3 us; 12 sequences with a head of 256 24.6 / 28.7)
   p->join_rows = tiles <= 256 ? 4 : kRowTile;
   p->waves = waves_in(p->c.d, bytes_of, !p->cut && tiles < 256);
   p->resident = 256 * std::max(1, 4 * waves_of(p->c.d, bytes_of, groups, p->waves) / p->waves);
-  p->least = 8 * p->waves;                           // (two steps a wave)
+  const int64_t least = 8 * p->waves;                // (two steps a wave)
   p->most_units = static_cast<int>(steps) * (2 + groups);
   // few tiles are cut into p->resident pieces at most, others into as many more than they are
-  auto pieces_of = [&](int64_t n) { return std::min(n + p->resident, n * (6 * steps / p->least + 2)); };
+  auto pieces_of = [&](int64_t n) { return std::min(n + p->resident, n * (6 * steps / least + 2)); };
   p->groups = p->cut ? pieces_of(tiles) : tiles;
+  // all tiles' units, each rounded up, stay below 2^31 (where some are not counted one by one there are
+  // more tiles or longer ones than pieces_of's second bound is for; pieces of 8 and more keep to the first)
+  p->unit_shift = 0;
+  while ((tiles * steps * (2 + groups) >> p->unit_shift) + tiles > 0x50000000) ++p->unit_shift;
+  p->least = static_cast<int>(std::max<int64_t>(8, least >> p->unit_shift));
   // (of more tiles than are cut, as for the most that are: a workspace serves every smaller batch)
   if (steps <= 64) return 16;
-  const int64_t n = p->cut ? tiles : std::min<int64_t>(tiles, std::max<int64_t>(511, 4 * steps));
+  const int64_t most = steps > 256 ? kCutTiles * p->c.heads : 4 * steps;
+  const int64_t n = p->cut ? tiles : std::min<int64_t>(tiles, std::max<int64_t>(511, most));
   return static_cast<size_t>(pieces_of(n)) * p->tile_rows * (p->c.d + 2) * sizeof(float) + static_cast<size_t>(n) * 16 + 16;
 }
 
@@ -985,8 +1002,6 @@ bool plan_tree(TreeParams* p, size_t* bytes) {
   const int64_t all_steps = steps_of(p->max_kv);
   int64_t steps = all_steps;
   if (p->window) steps = steps_of(std::min<int64_t>(p->max_kv, static_cast<int64_t>(p->window) + p->max_q + kUnit));
-  // units are counted in 32 bits
-  if (static_cast<int64_t>(p->B) * ((rows + kRowTile - 1) / kRowTile) * p->c.heads * 8 * all_steps > 0x50000000) return false;
   // Rows share a walk over the tokens where there is work for every compute unit; where there is not, tiles of
   // fewer rows end sooner.
   const int most = most_groups(p->c.d, p->dtype == CTS_F32);
@@ -995,11 +1010,11 @@ bool plan_tree(TreeParams* p, size_t* bytes) {
   for (int g = 1; g <= most && (g == 1 || rows > g / 2 * kRowTile); g *= 2) {
     *bytes = std::max(*bytes, plan_groups(p, g, all_steps));         // (whichever is taken, with any window)
     const int64_t tiles = static_cast<int64_t>(p->B) * p->subs * p->c.heads;
-    if (tiles + p->resident > max_groups(64 * kWaves) || tiles > max_groups(kJoinThreads)) return false;
-    if (!groups && (tiles * steps <= kLittleWork || rows <= p->tile_rows || 2 * g > most)) groups = g;
+    const bool little = tiles <= kLittleWork && tiles * steps <= kLittleWork;
+    if (!groups && (little || rows <= p->tile_rows || 2 * g > most)) groups = g;
   }
   plan_groups(p, groups, steps);
-  return true;
+  return static_cast<int64_t>(p->B) * p->subs * p->c.heads + p->resident <= max_groups(64 * kWaves);
 }
 
 void place_tree(TreeParams* p, void* workspace) {

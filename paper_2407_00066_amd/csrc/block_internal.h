@@ -92,10 +92,11 @@ struct TreeParams : AttnParams {
   int tile_rows;
   Divider by_group;
   // whether tiles are cut along their tokens; if not, whether those with most work go first; workgroups; how many run
-  // at a time; units of work of a piece at least, of a tile at most; waves of a workgroup; rows of a workgroup that joins
+  // at a time; units of work of a piece at least, of a tile at most, and 2^unit_shift of them that are counted as one; waves
+  // of a workgroup; rows of a workgroup that joins
   bool cut, ordered;
   int64_t groups;
-  int resident, least, most_units, waves, join_rows;
+  int resident, least, most_units, unit_shift, waves, join_rows;
 };
 bool plan_tree(TreeParams* p, size_t* bytes);
 void place_tree(TreeParams* p, void* workspace);
