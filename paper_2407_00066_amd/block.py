@@ -305,8 +305,8 @@ def kv_tree_attention(q, cache: KVCache, block_table, kv_len, mask, q_start=None
     are its last n cached tokens; a row sees the tokens before them (with a window, those
     less than that before positions [T], int32) and the drafts whose bits its
     mask [T, words] (int32, 32 drafts a word, the lowest bit first) has.  The rest
-    as for kv_attention; max_q (None: all rows of q, or as many as the mask has bits for)
-    is at most 512.  See cts_kv_tree_attention."""
+    as for kv_attention; max_q is at most 512, and the mask has a bit for each (None: all
+    rows of q, refused where these are more).  See cts_kv_tree_attention."""
     dev = cache.device
     r = _native.kv_tree_attention(_entry("cts_kv_tree_attention"), _entry("cts_kv_tree_attention_workspace_size"),
                                   _raw_stream(dev), dev, cache._at, q, block_table, kv_len, mask, q_start, max_q, max_kv,
@@ -329,6 +329,9 @@ def kv_tree_attention(q, cache: KVCache, block_table, kv_len, mask, q_start=None
             _dev(positions, "positions", dev, I32, (q.shape[0],))
         if workspace is not None:
             _dev(_binding._workspace(dev, 0, workspace), "workspace", dev, U8)
+        if max_q is None and q_start is not None and q.shape[0] > min(32 * mask.shape[1], 512):
+            raise ValueError("max_q is needed: without it all %d rows may be one sequence's drafts, of which the mask has bits "
+                             "for %d and a sequence at most 512" % (q.shape[0], 32 * mask.shape[1]))
         _refused(dev, "kv_tree_attention")
     _check(r[1], "cts_kv_tree_attention")
     return r[0]

@@ -377,8 +377,9 @@ PyObject* cts_marshal_kv_tree_attention(PyObject*, PyObject* const* a, Py_ssize_
     cts_attn_problem p{};
     p.T = int32(T); p.B = int32(B); p.n_q_heads = int32(heads); p.max_pages = int32(cols);
     p.dtype = dtype_code(dt);
-    // (no sequence has more drafts than rows, or than the mask has bits for)
-    p.max_q = a[10] != Py_None ? int32(a[10]) : a[9] == Py_None ? 1 : int32(std::max<int64_t>(std::min(T, 32 * words), 1));
+    // (all rows may be one sequence's: drafts past the mask's bits would be left out)
+    need(a[10] != Py_None || a[9] == Py_None || T <= std::min<int64_t>(32 * words, 512));
+    p.max_q = a[10] != Py_None ? int32(a[10]) : a[9] == Py_None ? 1 : int32(std::max<int64_t>(T, 1));
     p.max_kv = a[11] == Py_None ? int32(cols * c.page_size) : int32(a[11]);
     p.scale = static_cast<float>(number(a[12]));
     p.window = int32(a[13]);

@@ -61,3 +61,16 @@ def test_plan_of_much_work():
         return cts.kv_tree_attention_plan(q, cache, torch.zeros(1, 1).expand(B, cols), max_q, cols * 16)[1]
     assert how(64, 64, 65536) == "cut" and how(1024, 8, 65536) == "cut" and how(2048, 8, 65536) == "cut"
     assert how(2049, 8, 65536) == "whole" and how(1025, 31, 65536) == "whole"
+
+
+@pytest.mark.parametrize("rows,words", [(33, 1), (40, 1), (65, 2), (513, 20)])
+def test_max_q_is_asked_for(rows, words):
+    """(CPU tensors: refused before the device is.)"""
+    cache = cts.kv_cache(2, 16, 2, 64, device="cpu")
+    i32 = lambda *shape: torch.zeros(*shape, dtype=torch.int32)
+    args = [torch.zeros(rows, 2, 64), cache, i32(2, 2), i32(2), i32(rows, words)]
+    with pytest.raises(ValueError, match="max_q"):
+        cts.kv_tree_attention(*args, q_start=i32(3))
+    for kw in (dict(q_start=i32(3), max_q=32), dict()):
+        with pytest.raises(ValueError, match="GPU"):
+            cts.kv_tree_attention(*args, **kw)
