@@ -50,29 +50,38 @@ __device__ __forceinline__ At place(const KvCache& c, int64_t slot, uint32_t hea
 constexpr int kPieces = 2;                       // of a thread at a time (8191 tokens of 8 x 128 written: 1, 2, 4 pieces 11, 9.2, 10 us)
 struct Work { Divider ne; int tokens; };
 
-// Eight elements, eighth e of a head row, quantised into a slot.  The four threads of a block of 32
-// go together.
-__device__ __forceinline__ void store8(const KvCache& c, int64_t slot, int head, int e, bool value, const float* f) {
-  // the largest magnitude as an integer: it orders like the value, NaN above all
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(f[i]) & 0x7fffffffu);
+// A block's scale from `top`, the largest magnitude of each of its four threads, which go together: as an integer it
+// orders like the value, NaN above all.
+struct BlockScale { int s; bool finite; };
+__device__ __forceinline__ BlockScale block_scale(uint32_t top) {
   top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 1)));
   top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 2)));
   const bool finite = top < 0x7f800000u;
   // a mantissa from 1.75 on would round past 6: the next power of two then
-  const int s = finite ? min(252, max(1, static_cast<int>((top + (1u << 21)) >> 23) - 2)) : 255;
+  return {finite ? min(252, max(1, static_cast<int>((top + (1u << 21)) >> 23) - 2)) : 255, finite};
+}
+__device__ __forceinline__ uint32_t codes8(const float* f, BlockScale b) {
   uint32_t q = 0;
-  if (finite) {
-    const float unit = __uint_as_float(static_cast<uint32_t>(s) << 23);
+  if (b.finite) {
+    const float unit = __uint_as_float(static_cast<uint32_t>(b.s) << 23);
     q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, f[0], f[1], unit, 0);
     q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, f[2], f[3], unit, 1);
     q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, f[4], f[5], unit, 2);
     q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, f[6], f[7], unit, 3);
   }
+  return q;
+}
+
+// Eight elements, eighth e of a head row, quantised into a slot.
+__device__ __forceinline__ void store8(const KvCache& c, int64_t slot, int head, int e, bool value, const float* f) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(f[i]) & 0x7fffffffu);
+  const BlockScale b = block_scale(top);
+  const uint32_t q = codes8(f, b);
   const At at = place(c, slot, head, e, value);
   *reinterpret_cast<uint32_t*>((value ? c.vc : c.kc) + at.code) = q;
-  if ((e & 3) == 0) (value ? c.vs : c.ks)[at.scale] = static_cast<uint8_t>(s);
+  if ((e & 3) == 0) (value ? c.vs : c.ks)[at.scale] = static_cast<uint8_t>(b.s);
 }
 
 // Workgroup w's keys or values of the rows from `rows` on, `ld` apart, into their slots.
@@ -100,29 +109,17 @@ __device__ __forceinline__ void write_rows(const KvCache& c, const Work& work, i
 #pragma unroll
     for (int j = 0; j < kPieces; ++j) {
       if (slot[j] < 0 || slot[j] >= c.slots()) continue;
-      // (store8's steps once more: called here, the compiler moves 15 registers more a pass, and 8191 tokens of 8 x 128
-      // written and 8704 read take 18.7 us instead of 17.9)
-      // the largest magnitude as an integer: it orders like the value, NaN above all
+      // (store8 written out: its loop over elements in a function of its own costs 15 registers more a pass, and 8191 tokens
+      // of 8 x 128 written and 8704 read 18.7 us instead of 17.9)
       uint32_t top = 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(f[j][i]) & 0x7fffffffu);
-      top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 1)));
-      top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 2)));
-      const bool finite = top < 0x7f800000u;
-      // a mantissa from 1.75 on would round past 6: the next power of two then
-      const int s = finite ? min(252, max(1, static_cast<int>((top + (1u << 21)) >> 23) - 2)) : 255;
-      uint32_t q = 0;
-      if (finite) {
-        const float unit = __uint_as_float(static_cast<uint32_t>(s) << 23);
-        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, f[j][0], f[j][1], unit, 0);
-        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, f[j][2], f[j][3], unit, 1);
-        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, f[j][4], f[j][5], unit, 2);
-        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, f[j][6], f[j][7], unit, 3);
-      }
+      const BlockScale b = block_scale(top);
+      const uint32_t q = codes8(f[j], b);
       const int head = piece[j] >> shift, e = piece[j] & (per - 1);
       const At at = place(c, slot[j], head, e, value);
       *reinterpret_cast<uint32_t*>((value ? c.vc : c.kc) + at.code) = q;
-      if ((e & 3) == 0) (value ? c.vs : c.ks)[at.scale] = static_cast<uint8_t>(s);
+      if ((e & 3) == 0) (value ? c.vs : c.ks)[at.scale] = static_cast<uint8_t>(b.s);
     }
   }
 }
