@@ -14,7 +14,8 @@
  * nothing is allocated or synchronised, calls only enqueue work on `stream`,
  * every argument error is found on the host before any HIP call, T == 0 is
  * a no-op, and a call of more work than a launch has threads for (137 GB of keys
- * to write, 2^23 sequences x heads to attend to) is CTS_ERR_UNSUPPORTED.  Arrays are 16-byte aligned (int32 arrays 4, int64 arrays 8) and
+ * to write, 2^23 sequences x heads to attend to) is CTS_ERR_UNSUPPORTED.  Arrays
+ * are 16-byte aligned (int32 arrays 4, int64 arrays 8) and
  * rows of elements may lie further apart than they are long, as the slices of a
  * packed q/k/v output do: ld* are row strides in elements, multiples of 16
  * bytes, at least the row's length and at most 2^28.  dtype is CTS_BF16 or
@@ -75,7 +76,8 @@ int cts_kv_read(const cts_kv_cache* c, int32_t T, const int64_t* slots, void* k,
  * 0: all from the first).  For each query head h, with key/value head h /
  * (n_q_heads / n_heads):
  *     out[h] = sum_t w_t v_t,   w = softmax_t(scale q[h] . k_t)
- * A query that sees nothing (P < 0, kv_len 0) gives zeros.  q and out are
+ * A query that sees nothing (P < 0, kv_len 0) gives zeros, and so does one whose scores are
+ * all -inf (an infinity in it may make them so).  q and out are
  * [T][n_q_heads][head_dim] of dtype, rows ldq and ldo apart.
  * Arithmetic: scores, softmax and sums in fp32.  Cached elements are exact in
  * bf16 (bf16 matrix cores).  bf16: the weights w are rounded to bf16 for the

@@ -1,4 +1,4 @@
-// Device helpers of the attention kernels (attention.hip, attention_tile.hip).
+// Device helpers of the attention kernels (attention.hip, attention_tile.hip, attention_tree.hip).
 #pragma once
 
 #include "block_internal.h"

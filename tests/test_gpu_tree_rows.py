@@ -161,3 +161,55 @@ def test_pages_outside_the_cache(B, kvh, heads, most, cols, how):
     for b in range(B):
         at = slice(int(c["q_start"][b]), int(c["q_start"][b + 1]))
         assert torch.isnan(out[at]).all() if b in sick else torch.equal(out[at], clean[at]), b
+
+
+@pytest.mark.parametrize("B,kvh,heads,d,dtype,most,cols,how", [
+    (60, 4, 16, 128, "bf16", 16, 80, "whole"), (80, 2, 8, 64, "bf16", 16, 300, "cut"), (60, 4, 16, 128, "f32", 8, 80, "whole"),
+    (5, 2, 8, 128, "bf16", 16, 40, "whole")])
+def test_queries_that_are_no_numbers(B, kvh, heads, d, dtype, most, cols, how):
+    """A NaN or an infinity in a query makes that query's head NaN (zeros, where every score is -inf) and no bit of another
+    row different."""
+    c = _batch(B, kvh, heads, d, dtype, most, cols, 200)
+    assert _plan(c)[1] == how
+    clean = call(c)
+    q = c["q"].clone()
+    sick = [(r, r % heads) for r in range(1, len(q), 3)]
+    for i, (r, h) in enumerate(sick):
+        q[r, h, (7 * r) % d] = (float("nan"), float("inf"), float("-inf"))[i % 3]
+    say("kv_tree_attention of NaN queries, %s" % how)
+    out = call(c, q=q)
+    well = torch.ones(q.shape[:2], dtype=torch.bool, device="cuda")
+    for i, (r, h) in enumerate(sick):
+        well[r, h] = False
+        assert torch.isnan(out[r, h]).all() or i % 3 and not out[r, h].any()
+    assert torch.equal(out[well], clean[well])
+
+
+@pytest.mark.parametrize("most,cols,how", [(16, 80, "whole"), (16, 300, "cut")])
+def test_lengths_and_rows_outside_their_bounds(most, cols, how):
+    """A kv_len past max_kv counts as that, one below 0 as 0; rows are clamped to those that there are, and a sequence whose
+    end lies before its start has none."""
+    B, kvh, heads, d = (60, 4, 16, 128) if how == "whole" else (80, 2, 8, 64)
+    c = _batch(B, kvh, heads, d, "bf16", most, cols, 200)
+    assert _plan(c)[:2] == (64, how)
+    room, T = cols * 16, len(c["q"])
+    over = dict(c, n_kv=c["n_kv"].copy(), q_start=c["q_start"].copy())
+    over["n_kv"][[0, 7, 20]] = [-1, -2 ** 31, -5]
+    c["n_kv"][[0, 7, 20]] = 0
+    # a last sequence of all the table's tokens (pages that others hold too)
+    c["table"][B - 1], c["n_kv"][B - 1], over["n_kv"][B - 1] = np.arange(cols) % len(c["cache"][0]), room, 2 ** 31 - 1
+    over["table"] = c["table"]
+    over["q_start"][0], over["q_start"][-1] = -77, 2 ** 31 - 1
+    assert c["q_start"][0] == 0 and c["q_start"][-1] == T
+    say("kv_tree_attention of lengths past their bounds, %s" % how)
+    assert torch.equal(call(over), call(c))
+    check(c)
+    # sequence 3 has no rows, sequence 4 from where it begins, more than max_q: those past it stay as they were
+    back = dict(c, q_start=c["q_start"].copy())
+    back["q_start"][4] = back["q_start"][3] - 5
+    a = torch.full_like(c["q"], 5.0)
+    call(back, out=a)
+    lo, hi = int(back["q_start"][4]), int(back["q_start"][5])
+    assert hi - lo > most and bool((a[lo + most:hi] == 5).all()) and not bool((a[lo:lo + most] == 5).all(2).any())
+    same = torch.equal(a[hi:], call(c)[hi:])                     # (cut, the lengths of pieces follow from all work)
+    assert same or how == "cut"
