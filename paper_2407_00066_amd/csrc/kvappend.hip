@@ -61,6 +61,7 @@ template <typename T, int HEADS, bool NT> __device__ __forceinline__ void append
   const int64_t t = p.per_token(i);
   const int in_token = i - static_cast<int>(t) * p.per_token.d, group = in_token >> shift, e = in_token & (per - 1);
   const int64_t slot = p.slots[t];
+  const int pos0 = p.r.pos[t];
   const T* const row = static_cast<const T*>(p.r.in[1]) + t * p.r.ldi[1];
   const int half = p.r.rot / 2, first = 8 * e;
   const bool turns = first < p.r.rot, pairs = turns && !p.r.interleaved;
@@ -74,11 +75,11 @@ template <typename T, int HEADS, bool NT> __device__ __forceinline__ void append
   if (turns) {
     float c[8] = {}, s[8] = {};
     if (p.r.interleaved) {
-      angles<4>(p.r, t, first / 2, c, s);
+      angles<4>(p.r, t, pos0, first / 2, c, s);
 #pragma unroll
       for (int k = 0; k < HEADS; ++k) turn8<4>(p.r, e, c, s, f[k], g[k]);
     } else {
-      angles<8>(p.r, t, first < half ? first : first - half, c, s);
+      angles<8>(p.r, t, pos0, first < half ? first : first - half, c, s);
 #pragma unroll
       for (int k = 0; k < HEADS; ++k) turn8<8>(p.r, e, c, s, f[k], g[k]);
     }

@@ -60,9 +60,27 @@ __device__ __forceinline__ void turn(float& lo, float& hi, float c, float s) {
 // Cosines and sines of token t's pairs j0 .. j0 + N - 1 (N 4 or 8, j0 a multiple of N): 16 or 32 bytes of each
 // table for every axis that the pairs lie in, nearly always one or two (2003 tokens of 24 heads of 128 in
 // fp32, 64 elements turned on three axes: with a load for every pair 25.4 us, so 19.3).
-template <int N> __device__ __forceinline__ void angles(const RotaryParams& p, int64_t t, int j0, float* c, float* s) {
+// pos0: the token's position on the first axis, which the caller asks for before its rows.
+// The launch's arrays are read at indexes that the compiler knows, here and in turn_heads: at others it holds them all in
+// registers and finds an entry by comparing, 470 selects a thread (64 and 2000 tokens of 32 + 8 heads of 128
+// in bf16: 4.6 and 20.4 us, so 3.0 and 9.4).
+template <int N>
+__device__ __forceinline__ void angles(const RotaryParams& p, int64_t t, int pos0, int j0, float* c, float* s) {
+  if (p.axes == 1) {
+    const int row = min(max(pos0, 0), p.n_pos - 1);
+    const int64_t at = static_cast<int64_t>(row) * (p.rot / 2) + j0;
+#pragma unroll
+    for (int j = 0; j < N; j += 4) {
+      get<float, 4>(p.cos + at + j, c + j);
+      get<float, 4>(p.sin + at + j, s + j);
+    }
+    return;
+  }
+  static_assert(kRotaryMaxAxes == 4);
+  const int e0 = p.end[0], e1 = p.end[1], e2 = p.end[2], e3 = p.end[3];
+  auto end_of = [=](int a) { return a == 0 ? e0 : a == 1 ? e1 : a == 2 ? e2 : e3; };
   int axis = 0;
-  while (axis + 1 < p.axes && j0 >= p.end[axis]) ++axis;
+  while (axis + 1 < p.axes && j0 >= end_of(axis)) ++axis;
   for (int from = 0;;) {                          // pairs from here on are of this axis or a later one
     const int row = min(max(p.pos[static_cast<int64_t>(axis) * p.T + t], 0), p.n_pos - 1);
     const int64_t at = static_cast<int64_t>(row) * (p.rot / 2) + j0;
@@ -77,7 +95,7 @@ template <int N> __device__ __forceinline__ void angles(const RotaryParams& p, i
       c[j] = j >= from ? cv[j] : c[j];
       s[j] = j >= from ? sv[j] : s[j];
     }
-    from = p.end[axis] - j0;
+    from = end_of(axis) - j0;
     if (from >= N || ++axis >= p.axes) return;
   }
 }
@@ -97,6 +115,7 @@ __device__ __forceinline__ void turn_heads(const RotaryParams& p, int64_t t0, in
   const int j0 = piece * 8;                       // the first pair
   const int at0 = !turns ? p.rot + (piece - pieces) * 8 : p.interleaved ? 2 * j0 : j0;
   const int at1 = p.interleaved ? 2 * j0 + 8 : j0 + half;
+  const int pos0 = p.pos[t];
   float a[HEADS][16];
   T* o[HEADS];
 #pragma unroll
@@ -104,9 +123,10 @@ __device__ __forceinline__ void turn_heads(const RotaryParams& p, int64_t t0, in
     const int all = group + k * groups;
     o[k] = nullptr;
     if (all >= heads) continue;
-    const int which = all >= p.heads[0], head = which ? all - p.heads[0] : all;
-    const T* x = static_cast<const T*>(p.in[which]) + t * p.ldi[which] + static_cast<int64_t>(head) * p.d;
-    o[k] = static_cast<T*>(p.out[which]) + t * p.ldo[which] + static_cast<int64_t>(head) * p.d;
+    const bool key = all >= p.heads[0];
+    const int64_t head = key ? all - p.heads[0] : all;
+    const T* x = static_cast<const T*>(key ? p.in[1] : p.in[0]) + t * (key ? p.ldi[1] : p.ldi[0]) + head * p.d;
+    o[k] = static_cast<T*>(key ? p.out[1] : p.out[0]) + t * (key ? p.ldo[1] : p.ldo[0]) + head * p.d;
 #pragma unroll
     for (int e = 0; e < 8; e += N) get<T, N>(x + at0 + e, a[k] + e);
     if (turns)
@@ -115,13 +135,20 @@ __device__ __forceinline__ void turn_heads(const RotaryParams& p, int64_t t0, in
   }
   if (turns) {
     float c[8] = {}, s[8] = {};
-    angles<8>(p, t, j0, c, s);
+    angles<8>(p, t, pos0, j0, c, s);
 #pragma unroll
     for (int k = 0; k < HEADS; ++k)
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        if (p.interleaved) turn(a[k][2 * j], a[k][2 * j + 1], c[j], s[j]);
-        else turn(a[k][j], a[k][8 + j], c[j], s[j]);
+        if constexpr (HEADS <= 2) {                 // (four heads: selects cost more than both branches' code)
+          float& lo = p.interleaved ? a[k][2 * j] : a[k][j];
+          float& hi = p.interleaved ? a[k][2 * j + 1] : a[k][8 + j];
+          turn(lo, hi, c[j], s[j]);
+        } else if (p.interleaved) {
+          turn(a[k][2 * j], a[k][2 * j + 1], c[j], s[j]);
+        } else {
+          turn(a[k][j], a[k][8 + j], c[j], s[j]);
+        }
       }
   }
 #pragma unroll
