@@ -1,5 +1,5 @@
-"""cts_rotary beside a copy: it may not fall behind by far.  The bound is wide (the call takes two thirds of it), the
-times are the least of many replays."""
+"""cts_rotary beside a copy, and cts_kv_append beside the two calls that it stands for: neither may fall behind by far.
+The bounds are wide (the calls take two thirds of them), the times are the least of many replays."""
 import pytest
 import torch
 
@@ -48,3 +48,23 @@ def test_rotary_keeps_pace_with_a_copy(T, heads, kvh, d):
     turned = _least(lambda: cts.rotary(rows[:, :heads], rows[:, heads:heads + kvh], cos, sin, pos, q_out=q_out, k_out=k_out))
     say("copy %.1f us, rotary %.1f" % (copy, turned))
     assert turned <= 2 * copy
+
+
+@pytest.mark.parametrize("T,interleaved,dtype", [(1600, True, torch.float32), (1600, False, torch.float32), (1600, True, torch.bfloat16),
+                                                 (1600, False, torch.bfloat16), (64, False, torch.bfloat16)])
+def test_append_keeps_pace_with_its_parts(T, interleaved, dtype):
+    """One call of kv_append takes no longer than rotary and kv_write (0.6 to 0.8 of them; in fp32, interleaved, with streaming
+    stores 1.5)."""
+    rows, cos, sin, pos = _inputs(T, 32, 8, 128, dtype)
+    q, k, v = rows[:, :32], rows[:, 32:40], rows[:, 40:]
+    q_out, k_out = torch.empty(T, 32, 128, dtype=dtype, device="cuda"), torch.empty(T, 8, 128, dtype=dtype, device="cuda")
+    cache, slots = cts.kv_cache(T // 16 + 1, 16, 8, 128), torch.randperm(T, device="cuda")
+
+    def parts():
+        cts.rotary(q, k, cos, sin, pos, interleaved=interleaved, q_out=q_out, k_out=k_out)
+        cts.kv_write(cache, k_out, v, slots)
+    say("append beside rotary and write, T=%d %s interleaved=%d" % (T, dtype, interleaved))
+    two = _least(parts)
+    one = _least(lambda: cts.kv_append(cache, q, k, v, slots, cos, sin, pos, interleaved=interleaved, q_out=q_out))
+    say("parts %.1f us, append %.1f" % (two, one))
+    assert one <= 1.1 * two
