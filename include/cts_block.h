@@ -214,8 +214,8 @@ int cts_kv_tree_attention(const cts_attn_problem* p, const cts_kv_cache* c, cons
  * move as they are, and all of a sequence's are read before any is written, whatever the
  * path's order.  What lies outside a sequence's drafts or tokens, or on a page
  * outside the cache, is neither read nor written; tokens past n_path[b] keep what they hold.
- * kv_len itself is the caller's to set, to kv_len[b] - n + n_path[b].  Sequences whose tables share a page
- * of drafts leave either's tokens there. */
+ * kv_len itself is the caller's to set, to kv_len[b] - n + n_path[b].  Sequences whose
+ * tables share a page of drafts leave either's tokens there. */
 int cts_kv_keep(const cts_kv_cache* c, int32_t B, int32_t max_pages, const int32_t* block_table, const int32_t* kv_len,
                 const int32_t* q_start, int32_t max_path, const int32_t* path, const int32_t* n_path, void* stream);
 

@@ -10,11 +10,16 @@
 // zeros: what lies before the drafts is seen, what lies behind them is not, and 32 tokens' bits
 // are one shift wherever the drafts begin.
 //
-// 32 + 8 heads of 128 in bf16: 200 requests of 30 to 2000 tokens with 1 to 6 drafts 59 us, 4.0 TB/s of codes; 64 drafts
-// after 131 022 tokens and two like it 230 us, 853 TFLOP/s, bound by vector instructions beside the matrix
-// instructions: a step of 64 rows is 64 products (1024 cycles) and 267 others (2300 cycles in all with two waves a
-// SIMD).  16 rows a walk, which convert the codes four times as often: 427 us.  One tree of 7
-// over 709 tokens: 8.5 us, the chain of lengths, pages, codes and the waves' join.
+// In bf16 a weight is rounded to bf16 for the product with the values, and a row's length is the sum of the
+// rounded ones: one matrix instruction instead of the two or three that more parts of it would take, for an
+// error (2-norm) of 0.0021 to 0.0023 where the output's own rounding alone is 0.0017.
+//
+// 32 + 8 heads of 128 in bf16: 200 requests of 30 to 2000 tokens with 1 to 6 drafts 59.5 us, 3.8 TB/s of codes and
+// scales; 64, 31 and 50 drafts after 65 472, 39 970 and 131 022 tokens 228 us, 861 TFLOP/s, bound by vector
+// instructions beside the matrix instructions: a step of 64 rows is 64 products (1024 cycles) and 267 others
+// (2300 cycles in all with two waves a SIMD, as the waves time it).  16 rows a walk, which convert the codes four
+// times as often: 427 us.  One tree of 7 over 709 tokens: 8.5 us, the chain of lengths, pages, codes and the
+// waves' join.
 #include <algorithm>
 
 #include "attention_common.h"
@@ -68,7 +73,8 @@ __device__ __forceinline__ TreeTile of_lane(const TreeTile& t, int lane) {
 // Kinds of instructions to the scheduler.
 constexpr int kValu = 0x2, kMatrix = 0x8, kLdsRead = 0x100;
 
-// The maximum of a row that has seen nothing: finite, so that no step asks whether there is one.
+// The maximum of a row that has seen nothing: finite, so that no step asks whether there is one (scores below it weigh
+// nothing).
 constexpr float kNoMax = -3.0e38f;
 
 // What a wave holds of 16 rows (attention.hip).
@@ -101,7 +107,8 @@ template <int D> struct Step {
   static constexpr int kScales = D == 256 ? 2 : 1;           // loads of 4 bytes a lane for the scales
   static constexpr int kLoads = 2 * kPieces + kScales;
   static constexpr int kBytes = 2 * kPieces * 1024 + kScales * 256;
-  // (three: 200 small trees 63 -> 72 us, 64 x 8 drafts after 4000 tokens 68 -> 76; four: one workgroup a compute unit, 239 -> 370 over long documents)
+  // (three: 200 small trees 63 -> 72 us, 64 x 8 drafts after 4000 tokens 68 -> 76; four: one workgroup a compute
+  // unit, 239 -> 370 over long documents)
   static constexpr int kSlots = 2;
 };
 
@@ -391,8 +398,8 @@ __device__ __forceinline__ void attend(const TreeParams& p, const TreeTile& t, i
   const uint32_t ring_at = __builtin_amdgcn_readfirstlane(lds_at(ring));
   // Of two waves of a SIMD the older goes first, and the younger of two equal pieces ended a third later, alone for that
   // time: it goes first every other step (long documents: ends at 177 and 240 us, so at 221 and 232; always: 242 and 179).
-  // (Not where every tile has 16 rows, for whose short steps it costs more than it gives: 8 x 16 drafts after 2000 tokens 18.7 us,
-  // with it 19.5.)
+  // (Not where every tile has 16 rows, for whose short steps it costs more than it gives: 8 x 16 drafts after 2000 tokens
+  // 18.7 us, with it 19.5.)
   const bool younger = SHARED && p.cut && blockIdx.x >= 256;
   for (int it = 0; it < count; ++it) {
     if (younger) {
@@ -825,7 +832,8 @@ __device__ __forceinline__ void take(const TreeParams& p, const Piece& me, int p
 
 // Waves of a workgroup: eight where there are few, four, of which a compute unit takes more, where there are
 // many; shared memory holds the codes of eight waves of heads of 256, and queries in 32 bits beside those of four.
-// One tree over 709 tokens, eight waves or four: 8.8 / 9.5 us, eight in fp32 13.8 / 16.3; 200 small trees 93 / 63, 64 uneven ones 60 / 57.
+// One tree over 709 tokens, eight waves or four: 8.8 / 9.5 us, eight in fp32 13.8 / 16.3; 200 small trees 93 / 63, 64
+// uneven ones 60 / 57.
 constexpr int waves_in(int d, int bytes, bool few) { return d == 256 ? (bytes == 4 ? 4 : 8) : few ? 8 : 4; }
 // Waves of a SIMD that the registers are for.
 constexpr int waves_of(int d, int bytes, int rg, int waves) {
@@ -936,15 +944,16 @@ template <int D, typename TQ, int RG> void launch_tiles(const TreeParams& p, hip
 }
 
 // Steps of all tiles up to which tiles of fewer rows are taken (32 + 8 heads of 128, us with tiles of 64 rows / with this: 16
-// sequences of 16 drafts after 2000 tokens 28.1 / 22.5, 200 drafts after 1500 25.9 / 17.8, 8 x 16 in fp32 28.3 / 23.6; above it rows
-// have to share their steps: 64 x 8 after 900 20.9 / 24.0, 64 uneven trees 57 / 63, wide trees 58 / 75, 131 022 tokens 239 / 427).
+// sequences of 16 drafts after 2000 tokens 28.1 / 22.5, 200 drafts after 1500 25.9 / 17.8, 8 x 16 in fp32 28.3 / 23.6;
+// above it rows have to share their steps: 64 x 8 after 900 20.9 / 24.0, 64 uneven trees 57 / 63, wide trees 58 / 75,
+// long documents 239 / 427).
 constexpr int64_t kLittleWork = 16384;
 
 // Tiles (of a head) up to which they are cut: every piece is found by a look at all of them, so that finding them
-// takes the square of their number.  6 drafts each after 500 tokens, after 50 to 4000, and after 500 with one sequence of 16 000, bounds of
-// 16 384, 32 + 8 heads of 128, us cut / whole: 512 sequences 127 / 78, 200 / 158, 135 / 163; 1024 309 / 146, 384 / 251, 305 / 205; 2048
-// 839 / 301, 990 / 490, 848 / 297; 8192 9800 / 1290, 9500 / 1840, 9760 / 1140; 4 + 1 heads, 1024 56 / 25, 76 / 61, 66 / 129; 2048
-// 137 / 42, 169 / 89, 144 / 139; 4096 423 / 76, 440 / 142, 429 / 159.
+// takes the square of their number.  6 drafts each after 500 tokens, after 50 to 4000, and after 500 with one sequence of
+// 16 000, bounds of 16 384, 32 + 8 heads of 128, us cut / whole: 512 sequences 127 / 78, 200 / 158, 135 / 163; 1024 309 /
+// 146, 384 / 251, 305 / 205; 2048 839 / 301, 990 / 490, 848 / 297; 8192 9800 / 1290, 9500 / 1840, 9760 / 1140; 4 + 1 heads,
+// 1024 56 / 25, 76 / 61, 66 / 129; 2048 137 / 42, 169 / 89, 144 / 139; 4096 423 / 76, 440 / 142, 429 / 159.
 constexpr int64_t kCutTiles = 2048;
 
 template <int D, typename TQ> hipError_t launch(const TreeParams& p, hipStream_t s) {
@@ -968,13 +977,14 @@ static size_t plan_groups(TreeParams* p, int groups, int64_t steps) {
   const int64_t of_head = static_cast<int64_t>(p->B) * p->subs;
   // (more than a launch takes are refused if these tiles are chosen, and only need a workspace that does not fall)
   const int64_t tiles = std::min(of_head * p->c.heads, max_groups(64 * kWaves));
-  // Cut and whole, us: 12 sequences of up to 6000 tokens for one head of 256 24.6 / 56, 8 wide trees 58 / 93, 64 drafts after 8000 tokens
-  // 29 / 73, long documents 239 / 1013; with 512 tiles of up to 128 steps finding the pieces and joining them
-  // costs more than uneven ends: 51.6 / 45.
+  // Cut and whole, us: 12 sequences of up to 6000 tokens for one head of 256 24.6 / 56, 8 wide trees 58 / 93, 64 drafts
+  // after 8000 tokens 29 / 73, long documents 239 / 1013; with 512 tiles of up to 128 steps finding the pieces and joining
+  // them costs more than uneven ends: 51.6 / 45.
   p->cut = steps > 64 && of_head <= kCutTiles && (tiles < 512 || steps > std::min<int64_t>(256, tiles / 4));
   // (64 trees after 40 to 4000 tokens: 64 us in the batch's order, so 57)
   p->ordered = !p->cut && tiles > 256 && of_head <= kOrdered;
-  // (64 drafts after 8000 tokens, four rows of a tile a workgroup or 16: 29.4 / 32.3 us; 12 sequences with a head of 256 24.6 / 28.7)
+  // (64 drafts after 8000 tokens, four rows of a tile a workgroup or 16: 29.4 / 32.3 us; 12 sequences with a head of 256
+  // 24.6 / 28.7)
   p->join_rows = tiles <= 256 ? 4 : kRowTile;
   p->waves = waves_in(p->c.d, bytes_of, !p->cut && tiles < 256);
   p->resident = 256 * std::max(1, 4 * waves_of(p->c.d, bytes_of, groups, p->waves) / p->waves);

@@ -7,8 +7,8 @@
 // instead of twice, and its turned row is not written.  Workgroups take keys, values or queries.
 // A thread has 8 elements of a key: the 8 that they are turned with are another thread's, and
 // read again from the nearest cache instead of exchanged, so that any rot will do.  8191 tokens of 32 + 8 heads of
-// 128 in bf16: 39 us, 4.6 TB/s, where the caches hold none of them (rotary and write 33.8 + 9.7), 32 where they hold what fits; 33
-// tokens: 3.1 us (3.0 + 2.7), the chain of position, angles and rows.  (Calls in a graph.)
+// 128 in bf16: 39 us, 4.6 TB/s, where the caches hold none of them (rotary and write 33.8 + 9.7), 32 where they hold what
+// fits; 33 tokens: 3.1 us (3.0 + 2.7), the chain of position, angles and rows.  (Calls in a graph.)
 #include "kvblock.h"
 #include "rows.h"
 
@@ -136,12 +136,12 @@ template <typename T, int HEADS, bool NT> hipError_t append_launch(Append p, hip
 template <typename T> hipError_t append_typed(const Append& p, hipStream_t s) {
   // Two heads share their angles where that leaves workgroups enough, and large outputs are stored past the caches.
   // 32 + 8 heads of 128 in bf16, 1, 2 and 4 heads a thread with streaming stores: 200 tokens 3.4 / 4.0 / 5.2 us, 800 5.4 /
-  // 5.7 / 7.0, 1600 9.2 / 8.2 / 9.1, 4000 18.2 / 18.5 / 18.6, 16 000 74.8 / 75.4 / 80.2 (with ordinary stores, 2 heads: 1600 9.0,
-  // 4000 20.2, 16 000 78.3); 64 + 8 heads, 1600 13.1 / 11.9 / 12.5; 20 + 4 on three axes 9.4 / 8.2 / 8.4.
-  // In fp32 a thread's 16-byte stores lie 32 or 64 bytes apart, which streaming stores do not gather, and one head's
-  // rows are as long as two in bf16.  One head with ordinary stores, so, two with streaming ones: 1600 tokens of 32 + 8 heads of
-  // 128 14.1 / 18.4 us, interleaved 17.3 / 34.3, 16 000 131 / 173 and 152 / 354, of 64 + 8 219 / 308, of 8 + 1 heads of 64 15.1 / 20.9;
-  // of 20 + 4 on three axes, half of a head turned, 1600 12.1 / 13.3, 4000 28.0 / 27.4.
+  // 5.7 / 7.0, 1600 9.2 / 8.2 / 9.1, 4000 18.2 / 18.5 / 18.6, 16 000 74.8 / 75.4 / 80.2 (with ordinary stores, 2 heads:
+  // 1600 9.0, 4000 20.2, 16 000 78.3); 64 + 8 heads, 1600 13.1 / 11.9 / 12.5; 20 + 4 on three axes 9.4 / 8.2 / 8.4. In
+  // fp32 a thread's 16-byte stores lie 32 or 64 bytes apart, which streaming stores do not gather, and one head's rows
+  // are as long as two in bf16.  One head with ordinary stores, so, two with streaming ones: 1600 tokens of 32 + 8 heads
+  // of 128 14.1 / 18.4 us, interleaved 17.3 / 34.3, 16 000 131 / 173 and 152 / 354, of 64 + 8 219 / 308, of 8 + 1 heads
+  // of 64 15.1 / 20.9; of 20 + 4 on three axes, half of a head turned, 1600 12.1 / 13.3, 4000 28.0 / 27.4.
   if constexpr (sizeof(T) == 2) {
     const int64_t n = static_cast<int64_t>(p.r.T) * (p.r.heads[0] * (p.r.d / 16) + p.c.heads * (p.r.d / 8));
     if (n >= 512 * kThreads)
@@ -154,7 +154,8 @@ template <typename T> hipError_t append_typed(const Append& p, hipStream_t s) {
 // A workgroup takes one block of 32 elements of one head of a sequence: all of its accepted
 // tokens are read before any is written, so that no order and no repetition of them matters.
 // Codes and scales move as bytes, eight threads a token, without a barrier between heads.  64 sequences
-// of up to 33 drafts, 8 heads of 128: 5.2 us, one sequence 3.6 (calls in a graph): launch and the chain of path, page and codes.
+// of up to 33 drafts, 8 heads of 128: 5.2 us, one sequence 3.6 (calls in a graph): launch and the chain of path, page and
+// codes.
 constexpr int kKeepThreads = 128, kKeepParts = 8;
 
 struct alignas(16) Kept { uint32_t k[4], v[4]; };

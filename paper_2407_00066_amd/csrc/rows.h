@@ -59,7 +59,7 @@ __device__ __forceinline__ void turn(float& lo, float& hi, float c, float s) {
 
 // Cosines and sines of token t's pairs j0 .. j0 + N - 1 (N 4 or 8, j0 a multiple of N): 16 or 32 bytes of each
 // table for every axis that the pairs lie in, nearly always one or two (2003 tokens of 24 heads of 128 in
-// fp32, 64 elements turned on three axes: with a load for every pair 25.4 us, so 19.3).
+// fp32, 64 elements turned on three axes: with a load for every pair 20.3 us, so 13.6).
 // pos0: the token's position on the first axis, which the caller asks for before its rows.
 // The launch's arrays are read at indexes that the compiler knows, here and in turn_heads: at others it holds them all in
 // registers and finds an entry by comparing, 470 selects a thread (64 and 2000 tokens of 32 + 8 heads of 128

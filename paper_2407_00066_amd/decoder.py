@@ -47,7 +47,8 @@ class Batch:
     rows.  counts (host): tokens of each sequence in this step; kv_len (host):
     cached tokens after it; block_table: lists of pages, one a sequence.
     parents: the tokens are drafts, at most 512 of a sequence; draft_tree's parents for each
-    sequence (None: each token follows the one before)."""
+    sequence (None: each token follows the one before).  A step holds drafts or other tokens: longer
+    parts of prompts go into a batch of their own."""
 
     def __init__(self, adapter_of, cluster_of, n_adapters, n_clusters, counts, kv_len, block_table, page_size,
                  device="cuda", parents=None):
@@ -58,7 +59,8 @@ class Batch:
         trees = None
         if parents is not None:
             if len(parents) != len(counts) or any(p is not None and len(p) != n or n > 512 for n, p in zip(counts, parents)):
-                raise ValueError("parents must hold one for each of a sequence's tokens, at most 512")
+                raise ValueError("parents must hold one for each of a sequence's tokens, at most 512 (prompts go into a batch of "
+                                 "their own)")
             trees = [draft_tree(range(-1, n - 1) if p is None else p) for n, p in zip(counts, parents)]
         ids, pos, slots, start = [], [], [], [0]
         for b, (n, length) in enumerate(zip(counts, kv_len)):
